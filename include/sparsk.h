@@ -293,6 +293,150 @@ int sparsk_attention(const sparsk_attn_args *args /*host*/, void *scratch /*devi
 int sparsk_attention_static(const sparsk_attn_args *args /*host*/, void *cuda_stream, char *err /*host*/,
                             size_t err_len);
 
+/* ------------------------------------------------------------------ a paged cache
+ * For callers that share one pool of cache pages between their sequences.  A page holds page_size
+ * positions of every kv head; sequence i's position p lies in page block_table[i][p / page_size] at
+ * offset p % page_size, and "slot" p' = page * page_size + offset names the same place.  The four calls of a
+ * serving step, in their order: sparsk_page_map, sparsk_paged_append, sparsk_paged_attention,
+ * sparsk_sample.  They need no context; lengths, tables and settings are read on the device, so a
+ * captured step can be replayed while they change.  No counterpart in the paper: cache management of a
+ * server; the rows of a sequence are its refresh block (its pending positions and the
+ * current one, Algorithm 1, full-depth branch), or its one current position.
+ *
+ * Element types of these calls. */
+#define SPARSK_FP32 0
+#define SPARSK_BF16 1
+#define SPARSK_FP16 2
+#define SPARSK_E4M3 3 /* 8 bits, 3 of them significand: numbers of magnitude up to 448 */
+
+/* Pages for new rows, and where each row goes.  Sequence i holds seq_len[i] positions and gets
+ * seq_rows[i] >= 0 new ones, or has ended (seq_rows[i] == -1).  Free pages wait in a queue in a ring:
+ * ring[(queue[0] + t) % ring_size], t < queue[1].  Pages a sequence needs beyond those it has are
+ * taken from the head of the queue, sequence by sequence and block by block, and entered in its row of the table;
+ * the pages of a sequence that has ended go to the tail in the same order (a later call may hand them
+ * out; its row of the table is left as it was).  Row r of the step is row r - row_start[i] of
+ * sequence i, at position row_pos[r] = seq_len[i] + r - row_start[i] and slot slot_map[r]; entries of rows that
+ * the step does not have, up to max_rows, are set to -1, which sparsk_paged_append leaves out.
+ * All or nothing: *status is 0, or a sum of SPARSK_PAGES_* codes, and then no page has moved,
+ * lengths and queue are handed on as they came, row_start is 0 and every row -1.
+ * The new lengths and the new queue are written to arrays of their own (seq_len_out, queue_out must not
+ * overlap seq_len, queue), so that the call can be repeated; block_table and ring are changed in place.
+ * Page ids are the caller's and not looked at.  Enqueued on `cuda_stream`; SPARSK_EINVAL for NULL
+ * pointers, sizes below one (max_rows: below zero) or overlapping lengths or queues,
+ * SPARSK_ECAPACITY for more than SPARSK_MAX_MAP_SEQS sequences. */
+#define SPARSK_PAGES_SHORT 1  /* fewer free pages than needed                                     */
+#define SPARSK_PAGES_TABLE 2  /* a sequence needs more than max_blocks pages                      */
+#define SPARSK_PAGES_ROWS 4   /* more new rows than max_rows                                      */
+#define SPARSK_PAGES_BAD 8    /* a negative length, rows below -1, a queue that its ring cannot hold */
+#define SPARSK_MAX_MAP_SEQS 16384
+typedef struct {
+    const int32_t *seq_len, *seq_rows; /* [n_seqs]                                              */
+    int32_t *block_table;              /* [n_seqs][max_blocks], rows table_stride numbers apart */
+    int32_t *ring;                     /* [ring_size]                                           */
+    const int32_t *queue;              /* [2]: head, count                                      */
+    int32_t *seq_len_out, *queue_out;  /* [n_seqs], [2]                                         */
+    int32_t *row_start;                /* [n_seqs + 1]                                          */
+    int32_t *row_seq, *row_pos;        /* [max_rows]                                            */
+    int64_t *slot_map;                 /* [max_rows]                                            */
+    int32_t *status;                   /* [1]                                                   */
+    int64_t table_stride;
+    int32_t n_seqs, max_blocks, page_size, ring_size, max_rows;
+} sparsk_page_map_args;
+int sparsk_page_map(const sparsk_page_map_args *args /*host*/, void *cuda_stream);
+
+/* The pool of a paged cache: keys and values of one layer, of the same type, shape and strides.
+ * Element (page, head, position, dim) lies at page * page_stride + head * head_stride + position *
+ * pos_stride + dim, so heads may lie before or behind the positions of a page.  Both base
+ * pointers and (in bytes) all three strides are multiples of 16.  With scales, a stored number stands for itself
+ * times its head's scale. */
+typedef struct {
+    void *k, *v;                    /* device                                   */
+    const float *k_scale, *v_scale; /* [n_kv_heads] device, or NULL: 1          */
+    int64_t page_stride, head_stride, pos_stride; /* in elements                */
+    int32_t type;                   /* SPARSK_FP16, SPARSK_BF16 or SPARSK_E4M3  */
+    int32_t n_pages, n_kv_heads, page_size, head_dim /* 64 or 128 */;
+} sparsk_page_pool;
+
+/* New keys and values into their slots, and with a rotary table keys and queries turned to their
+ * positions on the way: with (c, s) = rope[row_pos[r]][j], numbers a = x[j] and b = x[j + head_dim / 2] of a
+ * head become a c - b s and b c + a s.  Arithmetic in fp32, one rounding to the type that is written; a
+ * number beyond the largest of fp16 or e4m3 is stored as that, NaN as NaN.  Rows whose slot is
+ * negative or outside the pool are not stored (their queries are turned all the same); with a table, rows
+ * whose position is outside it are neither stored nor turned.  Two rows of one call must not have
+ * the same slot: which of their numbers stay is not defined.  q and q_out may be the same memory (equal strides and types).
+ * Enqueued on `cuda_stream`; SPARSK_EINVAL for NULL or misaligned pointers and sizes or types out of range. */
+typedef struct {
+    sparsk_page_pool pool;
+    const void *k, *v;         /* [n_rows][n_kv_heads][head_dim] of x_type, with the strides below         */
+    const void *q;             /* [n_rows][n_q_heads][head_dim] of x_type, or NULL                         */
+    void *q_out;               /* [n_rows][n_q_heads][head_dim] of q_out_type; NULL if q is                */
+    const int64_t *slot_map;   /* [n_rows]                                                                 */
+    const int32_t *row_pos;    /* [n_rows]; NULL if rope is                                                */
+    const float *rope;         /* [rope_len][head_dim / 2][2]: cosine, sine; NULL: nothing is turned       */
+    int64_t k_row_stride, k_head_stride, v_row_stride, v_head_stride; /* in elements                       */
+    int64_t q_row_stride, q_head_stride, q_out_row_stride, q_out_head_stride;
+    int32_t x_type;            /* SPARSK_FP32, SPARSK_BF16 or SPARSK_FP16                                  */
+    int32_t q_out_type;        /* SPARSK_BF16 or SPARSK_FP16                                               */
+    int32_t n_rows, n_q_heads, rope_len;
+} sparsk_paged_append_args;
+int sparsk_paged_append(const sparsk_paged_append_args *args /*host*/, void *cuda_stream);
+
+/* Attention of a step's new rows over a paged cache that holds them already.  Sequence i has rows
+ * [row_start[i], row_start[i + 1]) (row_start NULL: row i alone, n_rows = n_seqs), its last row at
+ * position seq_len[i] - 1, the others at the positions before: row j of R sees the first seq_len[i] - R + 1 + j positions
+ * (the causal block of Algorithm 1's full-depth branch).  Query head h reads kv head h / (n_q_heads / n_kv_heads).
+ *   out[r][h] = sum_p w_p v_p / sum_p w_p,  w_p = exp(scale * q.k_p - max),  lse[r][h] = max + log sum_p w_p
+ * A row that sees nothing gets zeros and an lse of minus infinity; rows behind the last sequence's are left as they
+ * were.  Positions that a row does not see, and what lies behind a sequence's end in its last page, may hold anything, infinities and
+ * NaN too.  Positions in a page whose id is outside [0, n_pages) are left out; a length beyond the table is
+ * cut at the table's end.  Scores, softmax and sums are held in fp32; queries meet fp16 and e4m3 pages as fp16 numbers (of magnitude
+ * 65,504 at most), bf16 pages as bf16 numbers.
+ * max_rows and max_len are what the caller knows of a sequence's most rows and largest length (0: nothing): they size the launch, results do
+ * not depend on them.  `scratch` (device, 256-byte aligned, >= sparsk_paged_attention_scratch_bytes) is overwritten;
+ * nothing in it needs clearing; two calls that may overlap on the GPU need scratch of their own.
+ * SPARSK_EINVAL for NULL or misaligned pointers, sizes, types or strides out of range. */
+typedef struct {
+    sparsk_page_pool pool;
+    const void *q;              /* [n_rows][n_q_heads][head_dim] of q_type (bf16; fp16 unless the pool is bf16), turned */
+    void *out;                  /* the same shape and type                                       */
+    float *lse;                 /* [n_rows][n_q_heads], natural logarithm, or NULL               */
+    const int32_t *block_table; /* [n_seqs][max_blocks], rows table_stride numbers apart         */
+    const int32_t *seq_len;     /* [n_seqs], new rows included                                   */
+    const int32_t *row_start;   /* [n_seqs + 1] or NULL                                          */
+    int64_t table_stride;
+    int64_t q_row_stride, q_head_stride, out_row_stride, out_head_stride; /* in elements         */
+    int32_t q_type, n_rows, n_seqs, max_blocks, n_q_heads, max_rows, max_len;
+    float scale;                /* 0: 1 / sqrt(head_dim)                                         */
+} sparsk_paged_attn_args;
+size_t sparsk_paged_attention_scratch_bytes(const sparsk_paged_attn_args *args /*host*/);
+int sparsk_paged_attention(const sparsk_paged_attn_args *args /*host*/, void *scratch /*device*/, size_t scratch_bytes,
+                           void *cuda_stream);
+
+/* A token for every row of logits, with settings of each row's own.  Over the ids in [id_lo[r], id_hi[r])
+ * whose logit is neither NaN nor minus infinity, in the order of falling logits (equal ones: lower id first), with
+ * w = exp((z - max z) / temperature): the first top_k ids stay (0 or less: all); of those the shortest prefix whose mass
+ * reaches top_p times theirs (1 or more: all); of those the ids with w >= min_p (0 or less: all); at least
+ * one.  The token is the first id at which the cumulative mass exceeds uniforms[r] (in [0, 1)) times the
+ * kept mass.  A temperature of 0 (or less, or NaN) takes the first id of the order.  logprob[r] (may be
+ * NULL) is the logarithm of the token's softmax(z / temperature) over all of the row's ids (temperature 1 where it is 0 or less).
+ * A row without ids gets -1 and minus infinity.  Settings are DEVICE arrays [n_rows]; NULL stands for temperature 1, no
+ * cut, all ids.  The masses are exact to about 2^-40 of the whole and do not depend on the order in which the GPU adds them: the same
+ * call draws the same token.  Logits are only read; rows lie row_stride elements apart.  Enqueued on `cuda_stream`;
+ * SPARSK_EINVAL for NULL or misaligned pointers, sizes below one or an unknown type, SPARSK_ECAPACITY for more ids
+ * than SPARSK_MAX_SAMPLE_IDS. */
+#define SPARSK_MAX_SAMPLE_IDS 262144
+typedef struct {
+    const void *logits;        /* [n_rows][n_ids] of type SPARSK_FP32, SPARSK_BF16 or SPARSK_FP16 */
+    const float *uniforms;     /* [n_rows]                                                        */
+    const float *temperature, *top_p, *min_p;
+    const int32_t *top_k, *id_lo, *id_hi;
+    int32_t *token;            /* [n_rows]                                                        */
+    float *logprob;            /* [n_rows] or NULL                                                */
+    int64_t row_stride;        /* in elements                                                     */
+    int32_t type, n_rows, n_ids;
+} sparsk_sample_args;
+int sparsk_sample(const sparsk_sample_args *args /*host*/, void *cuda_stream);
+
 /* Per-kernel timing for roofline reports.  sparsk_set_option(ctx, "time_kernel", c) with c =
  * 1 QKV, 2 attention, 3 O-projection, 4 gate/up, 5 down-projection, 6 exit head, 7 persistent layer-range kernel (8: all of them, see sparsk_kernel_time_by_class) brackets every
  * later launch of that class with CUDA events on the context's stream (up to 16384 launches; 0

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from typing import NamedTuple
 
 import numpy as np
 import torch
@@ -19,6 +20,7 @@ EXPORTS = ("sparsk_workspace_bytes", "sparsk_create", "sparsk_prefill", "sparsk_
            "sparsk_decode_step_host", "sparsk_reset_slot", "sparsk_import_kv", "sparsk_export_kv",
            "sparsk_set_len", "sparsk_slot_state", "sparsk_set_debug", "sparsk_set_option",
            "sparsk_kernel_time", "sparsk_kernel_time_by_class", "sparsk_check", "sparsk_phase_trace", "sparsk_attention", "sparsk_attention_scratch_bytes", "sparsk_attention_static", "sparsk_sampling_scratch_bytes", "sparsk_set_sampling", "sparsk_nucleus_sample",
+           "sparsk_page_map", "sparsk_paged_append", "sparsk_paged_attention_scratch_bytes", "sparsk_paged_attention", "sparsk_sample",
            "sparsk_launch_count", "sparsk_route_counts", "sparsk_conf_entropies", "sparsk_last_error", "sparsk_destroy")
 
 OK, EINVAL, ECAPACITY, ENOHEAD, ECUDA, ESTATE, ETIMEOUT = 0, -1, -2, -3, -4, -5, -6
@@ -54,6 +56,42 @@ class AttnArgs(C.Structure):
 
 class Weights(C.Structure):
     _fields_ = [("embed", C.c_void_p)] + [(n, _PP) for n in PER_LAYER]
+
+
+FP32, BF16, FP16, E4M3 = 0, 1, 2, 3
+PAGES_SHORT, PAGES_TABLE, PAGES_ROWS, PAGES_BAD = 1, 2, 4, 8
+
+
+class PageMapArgs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("seq_len", "seq_rows", "block_table", "ring", "queue", "seq_len_out", "queue_out",
+                                          "row_start", "row_seq", "row_pos", "slot_map", "status")] + [
+        ("table_stride", C.c_int64)] + [(n, C.c_int32) for n in ("n_seqs", "max_blocks", "page_size", "ring_size", "max_rows")]
+
+
+class PagePool(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale")] + [
+        (n, C.c_int64) for n in ("page_stride", "head_stride", "pos_stride")] + [
+        (n, C.c_int32) for n in ("type", "n_pages", "n_kv_heads", "page_size", "head_dim")]
+
+
+class PagedAppendArgs(C.Structure):
+    _fields_ = [("pool", PagePool)] + [(n, C.c_void_p) for n in ("k", "v", "q", "q_out", "slot_map", "row_pos", "rope")] + [
+        (n, C.c_int64) for n in ("k_row_stride", "k_head_stride", "v_row_stride", "v_head_stride", "q_row_stride",
+                                 "q_head_stride", "q_out_row_stride", "q_out_head_stride")] + [
+        (n, C.c_int32) for n in ("x_type", "q_out_type", "n_rows", "n_q_heads", "rope_len")]
+
+
+class PagedAttnArgs(C.Structure):
+    _fields_ = [("pool", PagePool)] + [(n, C.c_void_p) for n in ("q", "out", "lse", "block_table", "seq_len", "row_start")] + [
+        (n, C.c_int64) for n in ("table_stride", "q_row_stride", "q_head_stride", "out_row_stride", "out_head_stride")] + [
+        (n, C.c_int32) for n in ("q_type", "n_rows", "n_seqs", "max_blocks", "n_q_heads", "max_rows", "max_len")] + [
+        ("scale", C.c_float)]
+
+
+class SampleArgs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("logits", "uniforms", "temperature", "top_p", "min_p", "top_k", "id_lo", "id_hi",
+                                          "token", "logprob")] + [
+        ("row_stride", C.c_int64)] + [(n, C.c_int32) for n in ("type", "n_rows", "n_ids")]
 
 
 _lib = None
@@ -107,6 +145,14 @@ def load():
     L.sparsk_set_sampling.argtypes = [vp, C.c_float, C.c_float, vp, vp, C.c_size_t]
     L.sparsk_nucleus_sample.restype = C.c_int
     L.sparsk_nucleus_sample.argtypes = [vp, vp, vp, C.c_int32, C.c_int32, C.c_int32, C.c_float, C.c_float, vp, vp]
+    for name in ("sparsk_page_map", "sparsk_paged_append", "sparsk_sample"):
+        f = getattr(L, name)
+        f.restype = C.c_int
+        f.argtypes = [vp, vp]   # (addresses again)
+    L.sparsk_paged_attention_scratch_bytes.restype = C.c_size_t
+    L.sparsk_paged_attention_scratch_bytes.argtypes = [vp]
+    L.sparsk_paged_attention.restype = C.c_int
+    L.sparsk_paged_attention.argtypes = [vp, vp, C.c_size_t, vp]
     L.sparsk_phase_trace.restype = C.c_int
     L.sparsk_phase_trace.argtypes = [vp, C.POINTER(C.c_int64), C.c_int32]
     L.sparsk_kernel_time_by_class.restype = C.c_int
@@ -212,6 +258,182 @@ def nucleus_sample(logits: torch.Tensor, uniforms: torch.Tensor, modality: torch
 
 def attention_scratch_bytes(n_rows: int, n_q_heads: int, head_dim: int) -> int:
     return load().sparsk_attention_scratch_bytes(n_rows, n_q_heads, head_dim)
+
+
+# ------------------------------------------------------------------ a paged cache
+_TYPES = {torch.float32: FP32, torch.bfloat16: BF16, torch.float16: FP16, torch.float8_e4m3fn: E4M3}
+
+
+class PageMap(NamedTuple):
+    """What page_map writes: lengths and queue after the step, and of every row its sequence, position and slot."""
+    seq_len: torch.Tensor
+    queue: torch.Tensor
+    row_start: torch.Tensor
+    row_seq: torch.Tensor
+    row_pos: torch.Tensor
+    slot_map: torch.Tensor
+    status: torch.Tensor
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise SparskError(EINVAL, what)
+
+
+def _vec(t: torch.Tensor, dtype, n: int, dev: int, what: str) -> int:
+    """Address of a contiguous array of at least n numbers on device `dev`."""
+    if t.dtype is not dtype or t.get_device() != dev or t.numel() < n or not t.is_contiguous():
+        raise SparskError(EINVAL, f"{what}: a contiguous {dtype} array of at least {n} numbers on cuda:{dev} is wanted")
+    return t.data_ptr()
+
+
+def _launch(name: str, dev: int, *args):
+    """One entry point, on the current stream of device `dev` whichever device is current."""
+    if torch._C._cuda_getDevice() == dev:
+        rc = getattr(load(), name)(*args, torch._C._cuda_getCurrentRawStream(dev))
+    else:
+        with torch.cuda.device(dev):
+            rc = getattr(load(), name)(*args, torch._C._cuda_getCurrentRawStream(dev))
+    if rc != OK:
+        raise SparskError(rc, name)
+
+
+def _page_pool(k: torch.Tensor, v: torch.Tensor, k_scale, v_scale) -> PagePool:
+    """Pools as [n_pages, n_kv_heads, page_size, head_dim]; pools whose positions lie before their heads come
+    transposed (`x.transpose(1, 2)`)."""
+    dev, shape, st = k.get_device(), k.shape, k.stride()
+    _need(dev >= 0 and v.get_device() == dev, "the pools are on one CUDA device")
+    _need(len(shape) == 4 and v.shape == shape and v.stride() == st and v.dtype is k.dtype, "pools of one shape, layout and type")
+    _need(st[3] == 1, "a head's numbers are contiguous")
+    ks = None if k_scale is None else _vec(k_scale, torch.float32, shape[1], dev, "k_scale")
+    vs = None if v_scale is None else _vec(v_scale, torch.float32, shape[1], dev, "v_scale")
+    return PagePool(k.data_ptr(), v.data_ptr(), ks, vs, st[0], st[1], st[2], _TYPES.get(k.dtype, -1), *shape)
+
+
+def _rows(t: torch.Tensor, n: int, heads: int, head_dim: int, dev: int, what: str):
+    """(address, row stride, head stride) of [n, heads, head_dim]."""
+    st = t.stride()
+    if t.shape != (n, heads, head_dim) or st[2] != 1 or t.get_device() != dev:
+        raise SparskError(EINVAL, f"{what}: [{n}, {heads}, {head_dim}] on cuda:{dev}, the last dimension contiguous, is wanted")
+    return t.data_ptr(), st[0], st[1]
+
+
+def _table(t: torch.Tensor, n: int, dev: int):
+    st = t.stride()
+    _need(t.dtype is torch.int32 and t.dim() == 2 and t.shape[0] >= n and st[1] == 1 and t.get_device() == dev,
+          "block_table: int32 [sequences, blocks], a row's entries contiguous")
+    return t.data_ptr(), st[0], t.shape[1]
+
+
+def page_map(lens: torch.Tensor, rows: torch.Tensor, block_table: torch.Tensor, ring: torch.Tensor, old_queue: torch.Tensor,
+             page_size: int, *, max_rows: int | None = None, seq_len=None, queue=None, row_start=None, row_seq=None, row_pos=None,
+             slot_map=None, status=None) -> PageMap:
+    """sparsk_page_map: pages for rows[i] new rows behind the lens[i] positions of every sequence (-1: the sequence has
+    ended, its pages go back), and each new row's sequence, position and slot.  block_table and ring are changed in place; results go
+    to the keyword arrays (as many rows as row_seq has), or to new ones of `max_rows` rows.  The status stays on
+    the device: 0, or PAGES_* codes, and then nothing has moved."""
+    dev, n = lens.get_device(), lens.shape[0]
+    _need(dev >= 0, "the lengths are on a CUDA device")
+    _need(row_seq is not None or max_rows is not None, "max_rows or row_seq says how many rows the step may have")
+    m = row_seq.shape[0] if row_seq is not None else int(max_rows)
+    new = lambda k, dtype=torch.int32: torch.empty(k, dtype=dtype, device=lens.device)  # noqa: E731
+    out = PageMap(seq_len if seq_len is not None else new(n), queue if queue is not None else new(2),
+                  row_start if row_start is not None else new(n + 1), row_seq if row_seq is not None else new(m),
+                  row_pos if row_pos is not None else new(m), slot_map if slot_map is not None else new(m, torch.int64),
+                  status if status is not None else new(1))
+    table, stride, blocks = _table(block_table, n, dev)
+    i32 = torch.int32
+    a = PageMapArgs(_vec(lens, i32, n, dev, "lens"), _vec(rows, i32, n, dev, "rows"), table, _vec(ring, i32, 1, dev, "ring"),
+                    _vec(old_queue, i32, 2, dev, "old_queue"), _vec(out.seq_len, i32, n, dev, "seq_len"),
+                    _vec(out.queue, i32, 2, dev, "queue"), _vec(out.row_start, i32, n + 1, dev, "row_start"),
+                    _vec(out.row_seq, i32, m, dev, "row_seq"), _vec(out.row_pos, i32, m, dev, "row_pos"),
+                    _vec(out.slot_map, torch.int64, m, dev, "slot_map"), _vec(out.status, i32, 1, dev, "status"),
+                    stride, n, blocks, page_size, ring.shape[0], m)
+    _launch("sparsk_page_map", dev, C.addressof(a))
+    return out
+
+
+def paged_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, slot_map: torch.Tensor, *,
+                 q: torch.Tensor | None = None, q_out: torch.Tensor | None = None, row_pos: torch.Tensor | None = None,
+                 rope: torch.Tensor | None = None, k_scale=None, v_scale=None) -> torch.Tensor | None:
+    """sparsk_paged_append: k, v [n, n_kv_heads, head_dim] into their slots (int64 [n], -1: left out); with
+    `rope` [positions, head_dim / 2, 2] (cosine, sine; float32) keys and queries q [n, n_q_heads, head_dim] are turned to
+    their positions row_pos (int32 [n]).  Returns the turned queries (q_out, or new: q's type, bf16 for fp32)."""
+    pool = _page_pool(k_cache, v_cache, k_scale, v_scale)
+    dev, n, hk, hd = k_cache.get_device(), k.shape[0], pool.n_kv_heads, pool.head_dim
+    kp, krs, khs = _rows(k, n, hk, hd, dev, "k")
+    vp, vrs, vhs = _rows(v, n, hk, hd, dev, "v")
+    _need(v.dtype is k.dtype, "k and v are of one type")
+    qp = qo = rp = rt = None
+    qrs = qhs = qors = qohs = hq = length = 0
+    qot = BF16
+    if q is not None:
+        hq = q.shape[1]
+        qp, qrs, qhs = _rows(q, n, hq, hd, dev, "q")
+        _need(q.dtype is k.dtype, "q and k are of one type")
+        if q_out is None:
+            q_out = torch.empty((n, hq, hd), dtype=torch.bfloat16 if q.dtype is torch.float32 else q.dtype, device=q.device)
+        qo, qors, qohs = _rows(q_out, n, hq, hd, dev, "q_out")
+        qot = _TYPES.get(q_out.dtype, -1)
+    if rope is not None:
+        _need(row_pos is not None and rope.dim() == 3 and rope.shape[1:] == (hd // 2, 2),
+              "rope: [positions, head_dim / 2, 2], and row_pos with it")
+        length = rope.shape[0]
+        rt, rp = _vec(rope, torch.float32, 1, dev, "rope"), _vec(row_pos, torch.int32, n, dev, "row_pos")
+    a = PagedAppendArgs(pool, kp, vp, qp, qo, _vec(slot_map, torch.int64, n, dev, "slot_map"), rp, rt, krs, khs, vrs, vhs, qrs, qhs,
+                        qors, qohs, _TYPES.get(k.dtype, -1), qot, n, hq, length)
+    if n:
+        _launch("sparsk_paged_append", dev, C.addressof(a))
+    return q_out
+
+
+def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor, seq_len: torch.Tensor,
+                    *, row_start: torch.Tensor | None = None, max_rows: int = 0, max_len: int = 0, scale: float = 0.0, k_scale=None,
+                    v_scale=None, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                    scratch: torch.Tensor | None = None) -> torch.Tensor:
+    """sparsk_paged_attention: rows q [n, n_q_heads, head_dim] (bf16 or fp16) of sequences whose seq_len (int32, new rows
+    included) positions lie in the pages of block_table (int32 [sequences, blocks]).  Sequence i has rows row_start[i]
+    to row_start[i + 1] - 1; without row_start every sequence has one.  max_rows and max_len, where known, size the launch.  `lse`
+    (float32 [n, n_q_heads]) receives the logarithms of the softmax sums."""
+    pool = _page_pool(k_cache, v_cache, k_scale, v_scale)
+    dev, n_seqs, (n, hq, hd) = k_cache.get_device(), seq_len.shape[0], q.shape
+    if out is None:
+        out = torch.empty((n, hq, hd), dtype=q.dtype, device=q.device)
+    _need(out.dtype is q.dtype and hd == pool.head_dim, "q and out are of one type, with the pool's head_dim")
+    qp, qrs, qhs = _rows(q, n, hq, hd, dev, "q")
+    op, ors, ohs = _rows(out, n, hq, hd, dev, "out")
+    table, stride, blocks = _table(block_table, n_seqs, dev)
+    a = PagedAttnArgs(pool, qp, op, None if lse is None else _vec(lse, torch.float32, n * hq, dev, "lse"), table,
+                      _vec(seq_len, torch.int32, n_seqs, dev, "seq_len"),
+                      None if row_start is None else _vec(row_start, torch.int32, n_seqs + 1, dev, "row_start"),
+                      stride, qrs, qhs, ors, ohs, _TYPES.get(q.dtype, -1), n, n_seqs, blocks, hq, max_rows, max_len, scale)
+    if n == 0:
+        return out
+    if scratch is None:
+        nbytes = load().sparsk_paged_attention_scratch_bytes(C.addressof(a))
+        _need(nbytes > 0, "sparsk_paged_attention: a size, type, stride or address that it does not take")
+        scratch = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+    _launch("sparsk_paged_attention", dev, C.addressof(a), _vec(scratch, torch.uint8, 1, dev, "scratch"), scratch.numel())
+    return out
+
+
+def sample(logits: torch.Tensor, uniforms: torch.Tensor, *, temperature=None, top_k=None, top_p=None, min_p=None, id_lo=None,
+           id_hi=None, token: torch.Tensor | None = None, logprob: torch.Tensor | None = None) -> torch.Tensor:
+    """sparsk_sample: one token (int32 [n]) for each row of logits [n, ids] (float32, bf16 or fp16), drawn with uniforms
+    (float32 [n]) by the row's own settings: float32 temperature, top_p, min_p and int32 top_k, id_lo, id_hi, each [n] on the
+    device, or None.  `logprob` (float32 [n]) receives the tokens' log probabilities before the cuts."""
+    dev, (n, ids) = logits.get_device(), logits.shape
+    _need(dev >= 0 and (ids == 1 or logits.stride(1) == 1), "logits: [rows, ids] on a CUDA device, a row contiguous")
+    if token is None:
+        token = torch.empty(n, dtype=torch.int32, device=logits.device)
+    f = lambda t, what: None if t is None else _vec(t, torch.float32, n, dev, what)  # noqa: E731
+    i = lambda t, what: None if t is None else _vec(t, torch.int32, n, dev, what)  # noqa: E731
+    a = SampleArgs(logits.data_ptr(), f(uniforms, "uniforms"), f(temperature, "temperature"), f(top_p, "top_p"), f(min_p, "min_p"),
+                   i(top_k, "top_k"), i(id_lo, "id_lo"), i(id_hi, "id_hi"), i(token, "token"), f(logprob, "logprob"),
+                   logits.stride(0), _TYPES.get(logits.dtype, -1), n, ids)
+    if n:
+        _launch("sparsk_sample", dev, C.addressof(a))
+    return token
 
 
 class Sparsk:

@@ -7,6 +7,7 @@
 #include "../../include/sparsk.h"
 #include "sparsk_attn.cuh"
 #include "sparsk_sample.cuh"
+#include "sparsk_settings_sample.cuh"
 #include "sparsk_step.cuh"
 
 using namespace sparsk;
@@ -131,4 +132,17 @@ extern "C" int sparsk_nucleus_sample(const float *logits, const float *uniforms,
     return launch_nucleus_sample(a, n, true, vocab_speech > 0, (cudaStream_t)cuda_stream, false, nullptr) == cudaSuccess
                ? SPARSK_OK
                : SPARSK_ECUDA;
+}
+
+extern "C" int sparsk_sample(const sparsk_sample_args *a, void *cuda_stream)
+{
+    if (!a || !a->logits || !a->uniforms || !a->token) return SPARSK_EINVAL;
+    if (a->type != SPARSK_FP32 && a->type != SPARSK_BF16 && a->type != SPARSK_FP16) return SPARSK_EINVAL;
+    if (a->n_rows < 1 || a->n_ids < 1 || a->row_stride < 0 || a->row_stride > (1ll << 40)) return SPARSK_EINVAL;
+    if ((uintptr_t)a->logits % (a->type == SPARSK_FP32 ? 4 : 2)) return SPARSK_EINVAL;
+    for (const void *p : {(const void *)a->uniforms, (const void *)a->temperature, (const void *)a->top_p, (const void *)a->min_p,
+                          (const void *)a->top_k, (const void *)a->id_lo, (const void *)a->id_hi, (const void *)a->token, (const void *)a->logprob})
+        if ((uintptr_t)p % 4) return SPARSK_EINVAL;
+    if (a->n_ids > SPARSK_MAX_SAMPLE_IDS) return SPARSK_ECAPACITY;
+    return launch_settings_sample(*a, (cudaStream_t)cuda_stream) == cudaSuccess ? SPARSK_OK : SPARSK_ECUDA;
 }

@@ -1,0 +1,159 @@
+// Entry points of the paged cache (C ABI in include/sparsk.h): page map, rows into pages, attention over pages.
+#include <algorithm>
+#include <climits>
+#include <cstdint>
+
+#include "../../include/sparsk.h"
+#include "sparsk_paged.cuh"
+#include "sparsk_paged_attn.cuh"
+
+using namespace sparsk;
+
+namespace {
+// [a, a + na) and [b, b + nb) share a byte
+bool overlap(const void *a, size_t na, const void *b, size_t nb)
+{
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return x < y + nb && y < x + na;
+}
+bool aligned(const void *p, size_t n) { return ((uintptr_t)p % n) == 0; }
+size_t type_bytes(int type) { return type == SPARSK_FP32 ? 4 : type == SPARSK_E4M3 ? 1 : 2; }
+
+int sm_count()
+{
+    static PerDevice<int> sms;
+    int &n = sms.here();
+    if (n == 0) {
+        int dev = 0;
+        if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) n = 0;
+    }
+    return n;
+}
+
+bool pool_ok(const sparsk_page_pool &p)
+{
+    if (!p.k || !p.v || !aligned(p.k, 16) || !aligned(p.v, 16) || !aligned(p.k_scale, 4) || !aligned(p.v_scale, 4)) return false;
+    if (p.type != SPARSK_FP16 && p.type != SPARSK_BF16 && p.type != SPARSK_E4M3) return false;
+    if (p.head_dim != 64 && p.head_dim != 128) return false;
+    if (p.n_pages < 1 || p.n_kv_heads < 1 || p.page_size < 1) return false;
+    const int64_t es = (int64_t)type_bytes(p.type);
+    for (int64_t s : {p.page_stride, p.head_stride, p.pos_stride})
+        if (s < 0 || s > (1ll << 30) || s * es % 16) return false;
+    return p.pos_stride >= p.head_dim;
+}
+// strides of [rows][heads][head_dim] numbers: any, as long as no address can overflow
+bool strides_ok(int64_t row, int64_t head) { return row >= 0 && head >= 0 && row < (1ll << 30) && head < (1ll << 30); }
+bool wide(const void *p, size_t es, int64_t row, int64_t head) { return aligned(p, 16) && row * es % 16 == 0 && head * es % 16 == 0; }
+}  // namespace
+
+// ------------------------------------------------------------------ page map
+extern "C" int sparsk_page_map(const sparsk_page_map_args *a, void *cuda_stream)
+{
+    if (!a || !a->seq_len || !a->seq_rows || !a->block_table || !a->ring || !a->queue || !a->seq_len_out || !a->queue_out ||
+        !a->row_start || !a->status)
+        return SPARSK_EINVAL;
+    if (a->max_rows < 0 || (a->max_rows > 0 && (!a->row_seq || !a->row_pos || !a->slot_map))) return SPARSK_EINVAL;
+    if (a->n_seqs < 1 || a->max_blocks < 1 || a->page_size < 1 || a->ring_size < 1) return SPARSK_EINVAL;
+    if (a->table_stride < a->max_blocks || a->table_stride > INT_MAX) return SPARSK_EINVAL;
+    for (const void *p : {(const void *)a->seq_len, (const void *)a->seq_rows, (const void *)a->block_table, (const void *)a->ring,
+                          (const void *)a->queue, (const void *)a->seq_len_out, (const void *)a->queue_out, (const void *)a->row_start,
+                          (const void *)a->row_seq, (const void *)a->row_pos, (const void *)a->status})
+        if (!aligned(p, 4)) return SPARSK_EINVAL;
+    if (!aligned(a->slot_map, 8)) return SPARSK_EINVAL;
+    if (a->n_seqs > SPARSK_MAX_MAP_SEQS) return SPARSK_ECAPACITY;
+    // blocks read the old lengths and the old queue while another writes the new ones
+    const size_t n = (size_t)a->n_seqs * 4;
+    for (const void *out : {(const void *)a->seq_len_out, (const void *)a->queue_out}) {
+        const size_t m = out == a->queue_out ? 8 : n;
+        if (overlap(out, m, a->seq_len, n) || overlap(out, m, a->seq_rows, n) || overlap(out, m, a->queue, 8)) return SPARSK_EINVAL;
+    }
+    const int smem = 3 * (a->n_seqs + 1) * (int)sizeof(int);
+    static PerDevice<bool> ready;
+    if (!ready.here()) {
+        if (cudaFuncSetAttribute(page_map_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 3 * (SPARSK_MAX_MAP_SEQS + 1) * (int)sizeof(int)) != cudaSuccess)
+            return SPARSK_ECUDA;
+        ready.here() = true;
+    }
+    // a block for every four rows a thread: the sums that each repeats cost about as much
+    const int grid = std::max(1, std::min(128, (a->max_rows + 4 * PM_THREADS - 1) / (4 * PM_THREADS)));
+    page_map_kernel<<<grid, PM_THREADS, smem, (cudaStream_t)cuda_stream>>>(*a);
+    return cudaGetLastError() == cudaSuccess ? SPARSK_OK : SPARSK_ECUDA;
+}
+
+// ------------------------------------------------------------------ rows into pages
+template <int XT>
+static void append_launch(const sparsk_paged_append_args &a, int row0, unsigned items, int vec, cudaStream_t st)
+{
+    const unsigned grid = (items + PA_THREADS - 1) / PA_THREADS;
+    if (a.pool.type == SPARSK_FP16) paged_append_kernel<XT, SPARSK_FP16><<<grid, PA_THREADS, 0, st>>>(a, row0, items, vec);
+    else if (a.pool.type == SPARSK_BF16) paged_append_kernel<XT, SPARSK_BF16><<<grid, PA_THREADS, 0, st>>>(a, row0, items, vec);
+    else paged_append_kernel<XT, SPARSK_E4M3><<<grid, PA_THREADS, 0, st>>>(a, row0, items, vec);
+}
+
+extern "C" int sparsk_paged_append(const sparsk_paged_append_args *a, void *cuda_stream)
+{
+    if (!a || !pool_ok(a->pool) || !a->k || !a->v || !a->slot_map || !aligned(a->slot_map, 8)) return SPARSK_EINVAL;
+    if (a->x_type != SPARSK_FP32 && a->x_type != SPARSK_BF16 && a->x_type != SPARSK_FP16) return SPARSK_EINVAL;
+    if (a->n_rows < 0 || !strides_ok(a->k_row_stride, a->k_head_stride) || !strides_ok(a->v_row_stride, a->v_head_stride)) return SPARSK_EINVAL;
+    const size_t es = type_bytes(a->x_type);
+    if (!aligned(a->k, es) || !aligned(a->v, es)) return SPARSK_EINVAL;
+    if (a->q) {
+        if (!a->q_out || a->n_q_heads < 1 || !strides_ok(a->q_row_stride, a->q_head_stride) || !strides_ok(a->q_out_row_stride, a->q_out_head_stride))
+            return SPARSK_EINVAL;
+        if ((a->q_out_type != SPARSK_BF16 && a->q_out_type != SPARSK_FP16) || !aligned(a->q, es) || !aligned(a->q_out, 2)) return SPARSK_EINVAL;
+    }
+    if (a->rope && (!a->row_pos || a->rope_len < 1 || !aligned(a->rope, 4) || !aligned(a->row_pos, 4))) return SPARSK_EINVAL;
+    int vec = 0;
+    if (wide(a->k, es, a->k_row_stride, a->k_head_stride)) vec |= 1;
+    if (wide(a->v, es, a->v_row_stride, a->v_head_stride)) vec |= 2;
+    if (a->q && wide(a->q, es, a->q_row_stride, a->q_head_stride)) vec |= 4;
+    if (a->q && wide(a->q_out, 2, a->q_out_row_stride, a->q_out_head_stride)) vec |= 8;
+    if (aligned(a->rope, 16)) vec |= 16;
+    const int64_t per_row = ((a->q ? (int64_t)a->n_q_heads : 0) + 2ll * a->pool.n_kv_heads) * (a->pool.head_dim / 16);
+    if (per_row > (1ll << 30)) return SPARSK_EINVAL;
+    const int most = (int)std::max<int64_t>(1, (1ll << 30) / per_row);  // rows whose items a launch can number
+    for (int row0 = 0; row0 < a->n_rows; row0 += std::min(most, a->n_rows - row0)) {
+        const unsigned items = (unsigned)(std::min(most, a->n_rows - row0) * per_row);
+        if (a->x_type == SPARSK_FP32) append_launch<SPARSK_FP32>(*a, row0, items, vec, (cudaStream_t)cuda_stream);
+        else if (a->x_type == SPARSK_BF16) append_launch<SPARSK_BF16>(*a, row0, items, vec, (cudaStream_t)cuda_stream);
+        else append_launch<SPARSK_FP16>(*a, row0, items, vec, (cudaStream_t)cuda_stream);
+        if (cudaGetLastError() != cudaSuccess) return SPARSK_ECUDA;
+    }
+    return SPARSK_OK;
+}
+
+// ------------------------------------------------------------------ attention over pages
+static bool paged_attn_ok(const sparsk_paged_attn_args *a)
+{
+    if (!a || !pool_ok(a->pool) || a->pool.page_size % 16) return false;
+    if (a->q_type != SPARSK_BF16 && !(a->q_type == SPARSK_FP16 && a->pool.type != SPARSK_BF16)) return false;
+    if (a->n_rows < 0 || a->n_seqs < 1 || a->max_blocks < 1 || a->n_q_heads < 1 || a->n_q_heads % a->pool.n_kv_heads) return false;
+    if (a->max_rows < 0 || a->max_len < 0 || (!a->row_start && a->n_rows != a->n_seqs)) return false;
+    if (!(a->scale >= 0.f) || !(a->scale < INFINITY)) return false;
+    if (a->table_stride < a->max_blocks || a->table_stride > INT_MAX) return false;
+    if ((int64_t)a->max_blocks * a->pool.page_size > INT_MAX) return false;
+    return strides_ok(a->q_row_stride, a->q_head_stride) && strides_ok(a->out_row_stride, a->out_head_stride);
+}
+
+extern "C" size_t sparsk_paged_attention_scratch_bytes(const sparsk_paged_attn_args *a)
+{
+    return paged_attn_ok(a) ? 256 : 0;
+}
+
+extern "C" int sparsk_paged_attention(const sparsk_paged_attn_args *a, void *scratch, size_t scratch_bytes, void *cuda_stream)
+{
+    if (!paged_attn_ok(a) || !a->q || !a->out || !a->block_table || !a->seq_len || !scratch || !aligned(scratch, 256)) return SPARSK_EINVAL;
+    if (!aligned(a->q, 2) || !aligned(a->out, 2) || !aligned(a->lse, 4) || !aligned(a->block_table, 4) || !aligned(a->seq_len, 4) ||
+        !aligned(a->row_start, 4))
+        return SPARSK_EINVAL;
+    if (scratch_bytes < sparsk_paged_attention_scratch_bytes(a)) return SPARSK_EINVAL;
+    if (a->n_rows == 0) return SPARSK_OK;
+    const float scale = a->scale > 0.f ? a->scale : 1.f / sqrtf((float)a->pool.head_dim);
+    const long long warps = (long long)a->n_rows * a->n_q_heads;
+    if (warps > INT_MAX) return SPARSK_EINVAL;
+    const int grid = (int)((warps + 3) / 4);
+    if (a->pool.head_dim == 64) paged_attn_simple_kernel<64><<<grid, 128, 0, (cudaStream_t)cuda_stream>>>(*a, scale);
+    else paged_attn_simple_kernel<128><<<grid, 128, 0, (cudaStream_t)cuda_stream>>>(*a, scale);
+    return cudaGetLastError() == cudaSuccess ? SPARSK_OK : SPARSK_ECUDA;
+}

@@ -1,0 +1,314 @@
+// A page pool's bookkeeping: which pages a step's new rows get, and the rows themselves into them.
+#pragma once
+
+#include <cuda_fp8.h>
+
+#include "../../include/sparsk.h"
+#include "sparsk_common.cuh"
+
+namespace sparsk {
+
+// ------------------------------------------------------------------ page map
+// With had = ceil(len / P), has = ceil((len + rows) / P): three running sums over the sequences (rows,
+// pages taken, pages given back) say everything; each entry written is then found on its own, by a
+// binary search for its sequence.  Nothing a block reads is written by another (a new row's page is read from
+// the queue and not from the table), so every block works the sums out for itself
+// and the blocks share the rows and pages without waiting for one another: one launch.
+// Latency is all there is to it (a step of 64 sequences writes about a kilobyte).
+constexpr int PM_THREADS = 1024;
+
+struct PageMapSums {
+    int rows, grow, back;
+};
+__device__ __forceinline__ int pm_blocks(int len, int page) { return (int)(((unsigned)len + (unsigned)page - 1u) / (unsigned)page); }
+
+// The largest i in [0, n) with first[i] <= x (first[0] = 0, ascending).
+__device__ __forceinline__ int pm_find(const int *first, int n, int x)
+{
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (first[mid] <= x) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+static __global__ void __launch_bounds__(PM_THREADS) page_map_kernel(sparsk_page_map_args a)
+{
+    extern __shared__ int pm_first[];  // [3][n_seqs + 1]: rows, pages taken, pages given back of the sequences before
+    __shared__ long long warp_sum3[3][PM_THREADS / 32];
+    __shared__ int warp_bad[PM_THREADS / 32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = a.n_seqs, P = a.page_size;
+    int *first_row = pm_first, *first_grow = pm_first + n + 1, *first_back = pm_first + 2 * (n + 1);
+    const int head = a.queue[0], count = a.queue[1];
+
+    // a thread's sequences lie side by side; sums in 64 bits, whatever the lengths say
+    const int per = (n + PM_THREADS - 1) / PM_THREADS, beg = min(tid * per, n), end = min(beg + per, n);
+    long long sum[3] = {0, 0, 0};
+    int bad = 0;
+    for (int i = beg; i < end; i++) {
+        const int len = a.seq_len[i], rows = a.seq_rows[i];
+        if (len < 0 || rows < -1) {
+            bad |= SPARSK_PAGES_BAD;
+            continue;
+        }
+        const long long after = (long long)len + (rows > 0 ? rows : 0), room = (long long)a.max_blocks * P;
+        if (after > room || after > INT_MAX) {
+            bad |= SPARSK_PAGES_TABLE;
+            continue;
+        }
+        const int had = pm_blocks(len, P);
+        sum[0] += rows > 0 ? rows : 0;
+        if (rows >= 0) sum[1] += pm_blocks((int)after, P) - had;
+        else sum[2] += had;
+    }
+    // exclusive sums over the threads
+    long long before[3];
+#pragma unroll
+    for (int q = 0; q < 3; q++) {
+        long long x = sum[q];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += y;
+        }
+        before[q] = x - sum[q];
+        if (lane == 31) warp_sum3[q][warp] = x;
+    }
+    bad = __reduce_or_sync(0xffffffffu, bad);
+    if (lane == 0) warp_bad[warp] = bad;
+    __syncthreads();
+    long long total[3] = {0, 0, 0};
+    bad = 0;
+    for (int w = 0; w < PM_THREADS / 32; w++) {
+#pragma unroll
+        for (int q = 0; q < 3; q++) {
+            if (w < warp) before[q] += warp_sum3[q][w];
+            total[q] += warp_sum3[q][w];
+        }
+        bad |= warp_bad[w];
+    }
+    if (head < 0 || head >= a.ring_size || count < 0 || count > a.ring_size) bad |= SPARSK_PAGES_BAD;
+    else {
+        if (total[1] > count) bad |= SPARSK_PAGES_SHORT;
+        if (total[2] > a.ring_size - count) bad |= SPARSK_PAGES_BAD;  // more pages than the ring has places
+    }
+    if (total[0] > a.max_rows) bad |= SPARSK_PAGES_ROWS;
+
+    const int step = gridDim.x * PM_THREADS, at = blockIdx.x * PM_THREADS + tid;
+    if (bad) {
+        for (int i = at; i < n; i += step) a.seq_len_out[i] = a.seq_len[i];
+        for (int i = at; i <= n; i += step) a.row_start[i] = 0;
+        for (int r = at; r < a.max_rows; r += step) {
+            a.row_seq[r] = a.row_pos[r] = -1;
+            a.slot_map[r] = -1;
+        }
+        if (at == 0) {
+            a.queue_out[0] = head;
+            a.queue_out[1] = count;
+            *a.status = bad;
+        }
+        return;
+    }
+    {
+        int b0 = (int)before[0], b1 = (int)before[1], b2 = (int)before[2];
+        for (int i = beg; i < end; i++) {
+            const int len = a.seq_len[i], rows = a.seq_rows[i], more = max(rows, 0), had = pm_blocks(len, P);
+            first_row[i] = b0;
+            first_grow[i] = b1;
+            first_back[i] = b2;
+            if (blockIdx.x == 0) {
+                a.row_start[i] = b0;
+                a.seq_len_out[i] = rows < 0 ? 0 : len + more;
+            }
+            b0 += more;
+            if (rows >= 0) b1 += pm_blocks(len + more, P) - had;
+            else b2 += had;
+        }
+    }
+    const int n_rows = (int)total[0], n_grow = (int)total[1], n_back = (int)total[2];
+    if (at == 0) {
+        a.row_start[n] = n_rows;
+        a.queue_out[0] = (int)(((long long)head + n_grow) % a.ring_size);
+        a.queue_out[1] = count - n_grow + n_back;
+        *a.status = 0;
+    }
+    __syncthreads();
+    const auto ring_at = [&](int t) { return (unsigned)(((long long)head + t) % a.ring_size); };
+    for (int r = at; r < a.max_rows; r += step) {
+        int seq = -1, pos = -1;
+        long long slot = -1;
+        if (r < n_rows) {
+            seq = pm_find(first_row, n, r);
+            const int len = a.seq_len[seq];
+            pos = len + (r - first_row[seq]);
+            const int block = (int)((unsigned)pos / (unsigned)P), had = pm_blocks(len, P);
+            const int page = block < had ? a.block_table[seq * a.table_stride + block] : a.ring[ring_at(first_grow[seq] + block - had)];
+            slot = (long long)page * P + (pos - block * P);
+        }
+        a.row_seq[r] = seq;
+        a.row_pos[r] = pos;
+        a.slot_map[r] = slot;
+    }
+    for (int t = at; t < n_grow; t += step) {
+        const int seq = pm_find(first_grow, n, t);
+        a.block_table[seq * a.table_stride + pm_blocks(a.seq_len[seq], P) + (t - first_grow[seq])] = a.ring[ring_at(t)];
+    }
+    for (int t = at; t < n_back; t += step) {
+        const int seq = pm_find(first_back, n, t);
+        a.ring[ring_at(count + t)] = a.block_table[seq * a.table_stride + (t - first_back[seq])];
+    }
+}
+
+// ------------------------------------------------------------------ rows into pages
+// A thread takes eight pairs (j, j + head_dim / 2) of one head of one row: two 16-byte reads and two writes of a
+// 16-bit type, and the pairs' cosines and sines once.  Bound by bytes where there are many rows (every number is
+// read and written once), by latency in a decode step.
+constexpr int PA_THREADS = 256;
+
+// A number beyond the type's largest is stored as that (an infinity in the cache would make every later score
+// of its head NaN), NaN stays NaN; the conversion to e4m3 does the same of itself.
+__device__ __forceinline__ float pa_clamp_fp16(float x)
+{
+    return x > 65504.f ? 65504.f : (x < -65504.f ? -65504.f : x);  // (a comparison with NaN is false)
+}
+template <int TYPE>
+__device__ __forceinline__ void pa_store8(void *p, const float (&v)[8], bool vec)
+{
+    if constexpr (TYPE == SPARSK_E4M3) {
+        uint32_t w[2];
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            const __nv_fp8x2_storage_t lo = __nv_cvt_float2_to_fp8x2(make_float2(v[i * 4], v[i * 4 + 1]), __NV_SATFINITE, __NV_E4M3);
+            const __nv_fp8x2_storage_t hi = __nv_cvt_float2_to_fp8x2(make_float2(v[i * 4 + 2], v[i * 4 + 3]), __NV_SATFINITE, __NV_E4M3);
+            w[i] = (uint32_t)lo | ((uint32_t)hi << 16);
+        }
+        *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
+    } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            w[i] = TYPE == SPARSK_BF16 ? pack_bf16x2(v[i * 2], v[i * 2 + 1]) : pack_h2(pa_clamp_fp16(v[i * 2]), pa_clamp_fp16(v[i * 2 + 1]));
+        if (vec) {
+            *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                reinterpret_cast<uint16_t *>(p)[i * 2] = (uint16_t)w[i];
+                reinterpret_cast<uint16_t *>(p)[i * 2 + 1] = (uint16_t)(w[i] >> 16);
+            }
+        }
+    }
+}
+template <int TYPE>
+__device__ __forceinline__ void pa_load8(const void *base, long long at, float (&v)[8], bool vec)
+{
+    if constexpr (TYPE == SPARSK_FP32) {
+        const float *p = reinterpret_cast<const float *>(base) + at;
+        if (vec) {
+            const float4 x = reinterpret_cast<const float4 *>(p)[0], y = reinterpret_cast<const float4 *>(p)[1];
+            v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i++) v[i] = p[i];
+        }
+    } else {
+        const uint16_t *p = reinterpret_cast<const uint16_t *>(base) + at;
+        uint32_t w[4];
+        if (vec) {
+            const uint4 x = *reinterpret_cast<const uint4 *>(p);
+            w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; i++) w[i] = (uint32_t)p[i * 2] | ((uint32_t)p[i * 2 + 1] << 16);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            if (TYPE == SPARSK_BF16) {
+                v[i * 2] = bf_lo(w[i]);
+                v[i * 2 + 1] = bf_hi(w[i]);
+            } else {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
+                v[i * 2] = f.x;
+                v[i * 2 + 1] = f.y;
+            }
+        }
+    }
+}
+
+// vec bits: 1 keys, 2 values, 4 queries, 8 turned queries may be read and written 16 bytes at a time, 16 the table
+template <int XT, int CT>
+static __global__ void __launch_bounds__(PA_THREADS) paged_append_kernel(sparsk_paged_append_args a, int row0, unsigned n_items, int vec)
+{
+    const unsigned idx = blockIdx.x * PA_THREADS + threadIdx.x;
+    if (idx >= n_items) return;
+    const int half = a.pool.head_dim >> 1, oct = half >> 3, Hk = a.pool.n_kv_heads, Hq = a.q ? a.n_q_heads : 0;
+    const unsigned per_row = (unsigned)(Hq + 2 * Hk) * oct;
+    const int row = row0 + (int)(idx / per_row), c = (int)(idx % per_row);
+    int head = c / oct;
+    const int j = (c % oct) * 8;
+    const int what = head < Hq ? 0 : head < Hq + Hk ? 1 : 2;  // query, key, value
+    head -= what == 0 ? 0 : what == 1 ? Hq : Hq + Hk;
+    long long slot = what == 0 ? 0 : a.slot_map[row];
+    const int pos = a.rope ? a.row_pos[row] : 0;
+    if (slot < 0 || slot >= (long long)a.pool.n_pages * a.pool.page_size || (a.rope && (pos < 0 || pos >= a.rope_len))) return;
+
+    float x[8], y[8];
+    const void *src = what == 0 ? a.q : what == 1 ? a.k : a.v;
+    const long long at = row * (what == 0 ? a.q_row_stride : what == 1 ? a.k_row_stride : a.v_row_stride) +
+                         head * (what == 0 ? a.q_head_stride : what == 1 ? a.k_head_stride : a.v_head_stride) + j;
+    const bool wide = vec & (what == 0 ? 4 : what == 1 ? 1 : 2);
+    pa_load8<XT>(src, at, x, wide);
+    pa_load8<XT>(src, at + half, y, wide);
+    if (a.rope && what != 2) {
+        const float *cs = a.rope + ((long long)pos * half + j) * 2;
+        float t[16];
+        if (vec & 16) {
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const float4 f = reinterpret_cast<const float4 *>(cs)[i];
+                t[i * 4] = f.x; t[i * 4 + 1] = f.y; t[i * 4 + 2] = f.z; t[i * 4 + 3] = f.w;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; i++) t[i] = cs[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const float u = x[i] * t[2 * i] - y[i] * t[2 * i + 1];
+            y[i] = y[i] * t[2 * i] + x[i] * t[2 * i + 1];
+            x[i] = u;
+        }
+    }
+    if (what == 0) {
+        const long long to = row * a.q_out_row_stride + head * a.q_out_head_stride + j;
+        uint16_t *q = reinterpret_cast<uint16_t *>(a.q_out) + to;
+        if (a.q_out_type == SPARSK_BF16) {
+            pa_store8<SPARSK_BF16>(q, x, vec & 8);
+            pa_store8<SPARSK_BF16>(q + half, y, vec & 8);
+        } else {
+            pa_store8<SPARSK_FP16>(q, x, vec & 8);
+            pa_store8<SPARSK_FP16>(q + half, y, vec & 8);
+        }
+        return;
+    }
+    const float *scale = what == 1 ? a.pool.k_scale : a.pool.v_scale;
+    if (scale) {
+        const float s = scale[head];
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            x[i] = __fdiv_rn(x[i], s);
+            y[i] = __fdiv_rn(y[i], s);
+        }
+    }
+    const long long page = (slot >> 32) ? slot / a.pool.page_size : (long long)((unsigned)slot / (unsigned)a.pool.page_size);
+    const int off = (int)(slot - page * a.pool.page_size);
+    const long long to = page * a.pool.page_stride + head * a.pool.head_stride + off * a.pool.pos_stride + j;
+    char *dst = reinterpret_cast<char *>(what == 1 ? a.pool.k : a.pool.v);
+    constexpr int ES = CT == SPARSK_E4M3 ? 1 : 2;
+    pa_store8<CT>(dst + to * ES, x, true);
+    pa_store8<CT>(dst + (to + half) * ES, y, true);
+}
+
+}  // namespace sparsk
