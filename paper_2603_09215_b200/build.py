@@ -8,7 +8,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsparsk.so")
-SOURCES = ["sparsk_api.cu", "sparsk_ops.cu", "sparsk_noalloc.cu", "sparsk_paged.cu"]
+SOURCES = ["sparsk_api.cu", "sparsk_ops.cu", "sparsk_noalloc.cu", "sparsk_paged.cu", "sparsk_paged_attn.cu"]
 
 
 def _stale() -> bool:

@@ -1,50 +1,14 @@
-// Entry points of the paged cache (C ABI in include/sparsk.h): page map, rows into pages, attention over pages.
+// Entry points of the paged cache (C ABI in include/sparsk.h): page map, rows into pages.
 #include <algorithm>
 #include <climits>
 #include <cstdint>
 
 #include "../../include/sparsk.h"
 #include "sparsk_paged.cuh"
-#include "sparsk_paged_attn.cuh"
+#include "sparsk_paged_host.h"
 
 using namespace sparsk;
 
-namespace {
-// [a, a + na) and [b, b + nb) share a byte
-bool overlap(const void *a, size_t na, const void *b, size_t nb)
-{
-    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-    return x < y + nb && y < x + na;
-}
-bool aligned(const void *p, size_t n) { return ((uintptr_t)p % n) == 0; }
-size_t type_bytes(int type) { return type == SPARSK_FP32 ? 4 : type == SPARSK_E4M3 ? 1 : 2; }
-
-int sm_count()
-{
-    static PerDevice<int> sms;
-    int &n = sms.here();
-    if (n == 0) {
-        int dev = 0;
-        if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) n = 0;
-    }
-    return n;
-}
-
-bool pool_ok(const sparsk_page_pool &p)
-{
-    if (!p.k || !p.v || !aligned(p.k, 16) || !aligned(p.v, 16) || !aligned(p.k_scale, 4) || !aligned(p.v_scale, 4)) return false;
-    if (p.type != SPARSK_FP16 && p.type != SPARSK_BF16 && p.type != SPARSK_E4M3) return false;
-    if (p.head_dim != 64 && p.head_dim != 128) return false;
-    if (p.n_pages < 1 || p.n_kv_heads < 1 || p.page_size < 1) return false;
-    const int64_t es = (int64_t)type_bytes(p.type);
-    for (int64_t s : {p.page_stride, p.head_stride, p.pos_stride})
-        if (s < 0 || s > (1ll << 30) || s * es % 16) return false;
-    return p.pos_stride >= p.head_dim;
-}
-// strides of [rows][heads][head_dim] numbers: any, as long as no address can overflow
-bool strides_ok(int64_t row, int64_t head) { return row >= 0 && head >= 0 && row < (1ll << 30) && head < (1ll << 30); }
-bool wide(const void *p, size_t es, int64_t row, int64_t head) { return aligned(p, 16) && row * es % 16 == 0 && head * es % 16 == 0; }
-}  // namespace
 
 // ------------------------------------------------------------------ page map
 extern "C" int sparsk_page_map(const sparsk_page_map_args *a, void *cuda_stream)
@@ -121,39 +85,4 @@ extern "C" int sparsk_paged_append(const sparsk_paged_append_args *a, void *cuda
         if (cudaGetLastError() != cudaSuccess) return SPARSK_ECUDA;
     }
     return SPARSK_OK;
-}
-
-// ------------------------------------------------------------------ attention over pages
-static bool paged_attn_ok(const sparsk_paged_attn_args *a)
-{
-    if (!a || !pool_ok(a->pool) || a->pool.page_size % 16) return false;
-    if (a->q_type != SPARSK_BF16 && !(a->q_type == SPARSK_FP16 && a->pool.type != SPARSK_BF16)) return false;
-    if (a->n_rows < 0 || a->n_seqs < 1 || a->max_blocks < 1 || a->n_q_heads < 1 || a->n_q_heads % a->pool.n_kv_heads) return false;
-    if (a->max_rows < 0 || a->max_len < 0 || (!a->row_start && a->n_rows != a->n_seqs)) return false;
-    if (!(a->scale >= 0.f) || !(a->scale < INFINITY)) return false;
-    if (a->table_stride < a->max_blocks || a->table_stride > INT_MAX) return false;
-    if ((int64_t)a->max_blocks * a->pool.page_size > INT_MAX) return false;
-    return strides_ok(a->q_row_stride, a->q_head_stride) && strides_ok(a->out_row_stride, a->out_head_stride);
-}
-
-extern "C" size_t sparsk_paged_attention_scratch_bytes(const sparsk_paged_attn_args *a)
-{
-    return paged_attn_ok(a) ? 256 : 0;
-}
-
-extern "C" int sparsk_paged_attention(const sparsk_paged_attn_args *a, void *scratch, size_t scratch_bytes, void *cuda_stream)
-{
-    if (!paged_attn_ok(a) || !a->q || !a->out || !a->block_table || !a->seq_len || !scratch || !aligned(scratch, 256)) return SPARSK_EINVAL;
-    if (!aligned(a->q, 2) || !aligned(a->out, 2) || !aligned(a->lse, 4) || !aligned(a->block_table, 4) || !aligned(a->seq_len, 4) ||
-        !aligned(a->row_start, 4))
-        return SPARSK_EINVAL;
-    if (scratch_bytes < sparsk_paged_attention_scratch_bytes(a)) return SPARSK_EINVAL;
-    if (a->n_rows == 0) return SPARSK_OK;
-    const float scale = a->scale > 0.f ? a->scale : 1.f / sqrtf((float)a->pool.head_dim);
-    const long long warps = (long long)a->n_rows * a->n_q_heads;
-    if (warps > INT_MAX) return SPARSK_EINVAL;
-    const int grid = (int)((warps + 3) / 4);
-    if (a->pool.head_dim == 64) paged_attn_simple_kernel<64><<<grid, 128, 0, (cudaStream_t)cuda_stream>>>(*a, scale);
-    else paged_attn_simple_kernel<128><<<grid, 128, 0, (cudaStream_t)cuda_stream>>>(*a, scale);
-    return cudaGetLastError() == cudaSuccess ? SPARSK_OK : SPARSK_ECUDA;
 }
