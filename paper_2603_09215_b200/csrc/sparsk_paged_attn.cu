@@ -70,7 +70,8 @@ bool paged_attn_ok(const sparsk_paged_attn_args *a)
     return strides_ok(a->q_row_stride, a->q_head_stride) && strides_ok(a->out_row_stride, a->out_head_stride);
 }
 
-// How many blocks of 16 query vectors share a read of a head's keys and values: as many as the most rows of a sequence have.
+// Tiles of 16 query vectors that a segment may have, for one read of a head's keys and values: as many as the most rows of a
+// sequence fill, four at most.
 int tiles_of(const sparsk_paged_attn_args *a)
 {
     const int64_t rows = !a->row_start ? 1 : a->max_rows > 0 ? a->max_rows : ((int64_t)a->n_rows + a->n_seqs - 1) / a->n_seqs;
@@ -91,13 +92,13 @@ Scratch scratch_of(const sparsk_paged_attn_args *a)
     return s;
 }
 
-template <int HD, int CT, int MT, bool P2>
+template <int HD, int CT, bool P2>
 cudaError_t launch(const PtArgs &p, const CUtensorMap &mk, const CUtensorMap &mv, int shares, bool join, cudaStream_t st)
 {
     static PerDevice<bool> ready;
     constexpr int smem = PtForm<HD, CT>::SMEM;
     if (!ready.here()) {
-        const cudaError_t e = cudaFuncSetAttribute(paged_attn_kernel<HD, CT, MT, P2>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        const cudaError_t e = cudaFuncSetAttribute(paged_attn_kernel<HD, CT, P2>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
         if (e != cudaSuccess) return e;
         ready.here() = true;
     }
@@ -111,28 +112,21 @@ cudaError_t launch(const PtArgs &p, const CUtensorMap &mk, const CUtensorMap &mv
     cfg.stream = st;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    cudaError_t e = cudaLaunchKernelEx(&cfg, paged_attn_kernel<HD, CT, MT, P2>, p, mk, mv);
+    cudaError_t e = cudaLaunchKernelEx(&cfg, paged_attn_kernel<HD, CT, P2>, p, mk, mv);
     if (e != cudaSuccess || !join) return e;
-    constexpr int JT = CT == SPARSK_E4M3 ? SPARSK_E4M3 : SPARSK_FP16;  // (which accumulators a lane holds)
-    cfg.gridDim = dim3(shares, 4 * MT);
+    cfg.gridDim = dim3(shares, 4 * p.tiles);
     cfg.blockDim = dim3(PJ_THREADS);
     cfg.dynamicSmemBytes = 0;
-    return cudaLaunchKernelEx(&cfg, paged_join_kernel<HD, JT, MT>, p, shares);
-}
-template <int HD, int CT, bool P2, class... A>
-cudaError_t launch_tiles(int mt, A... x)
-{
-    return mt == 1 ? launch<HD, CT, 1, P2>(x...) : mt == 2 ? launch<HD, CT, 2, P2>(x...) : launch<HD, CT, 4, P2>(x...);
+    return cudaLaunchKernelEx(&cfg, paged_join_kernel<HD, PtForm<HD, CT>::ES>, p, shares);
 }
 // A softmax weight is rounded to 16 bits where it meets the values; where that is no finer than the output's own
 // rounding, a second term carries the rest.
 template <int HD, class... A>
-cudaError_t launch_types(int pool_type, int q_type, int mt, A... x)
+cudaError_t launch_types(int pool_type, int q_type, A... x)
 {
-    if (pool_type == SPARSK_BF16) return launch_tiles<HD, SPARSK_BF16, true>(mt, x...);
-    if (pool_type == SPARSK_FP16)
-        return q_type == SPARSK_FP16 ? launch_tiles<HD, SPARSK_FP16, true>(mt, x...) : launch_tiles<HD, SPARSK_FP16, false>(mt, x...);
-    return q_type == SPARSK_FP16 ? launch_tiles<HD, SPARSK_E4M3, true>(mt, x...) : launch_tiles<HD, SPARSK_E4M3, false>(mt, x...);
+    if (pool_type == SPARSK_BF16) return launch<HD, SPARSK_BF16, true>(x...);
+    if (pool_type == SPARSK_FP16) return q_type == SPARSK_FP16 ? launch<HD, SPARSK_FP16, true>(x...) : launch<HD, SPARSK_FP16, false>(x...);
+    return q_type == SPARSK_FP16 ? launch<HD, SPARSK_E4M3, true>(x...) : launch<HD, SPARSK_E4M3, false>(x...);
 }
 }  // namespace
 
@@ -150,7 +144,7 @@ extern "C" int sparsk_paged_attention(const sparsk_paged_attn_args *a, void *scr
     const Scratch sc = scratch_of(a);
     if (scratch_bytes < sc.bytes) return SPARSK_EINVAL;
     if (a->n_rows == 0) return SPARSK_OK;
-    const int n_sm = sm_count(), mt = tiles_of(a);
+    const int n_sm = sm_count();
     if (n_sm == 0) return SPARSK_ECUDA;
     CUtensorMap mk, mv;
     if (!encode_pool(&mk, a->pool.k, a->pool) || !encode_pool(&mv, a->pool.v, a->pool)) return SPARSK_EINVAL;
@@ -168,21 +162,26 @@ extern "C" int sparsk_paged_attention(const sparsk_paged_attn_args *a, void *scr
     p.q_type = a->q_type; p.n_rows = a->n_rows; p.n_seqs = a->n_seqs; p.max_blocks = a->max_blocks;
     p.page_size = a->pool.page_size; p.n_pages = a->pool.n_pages;
     p.Hk = a->pool.n_kv_heads; p.G = a->n_q_heads / a->pool.n_kv_heads;
+    p.tiles = tiles_of(a);
+    p.g_inverse = (uint32_t)(((1ull << 32) + p.G - 1) / p.G);
+    p.g_limit = p.G == 1 ? 0 : (uint32_t)((1ull << 32) / p.G);  // (by 1 the plain division does)
     p.whole_boxes = PT_WHOLE;
+    p.q_words = aligned(a->q, 4) && a->q_row_stride % 2 == 0 && a->q_head_stride % 2 == 0;
+    p.out_words = aligned(a->out, 4) && a->out_row_stride % 2 == 0 && a->out_head_stride % 2 == 0;
     int shares = std::min(PT_CTAS * n_sm, PT_MAX_SHARES);
     bool join = true;
     if (a->max_len > 0) {
         // no more CTAs than there can be shares, and no join where no segment is long enough to be cut (if one is all
         // the same, its share takes the whole of it)
         const int64_t boxes = ((int64_t)a->max_len + PT_BOX - 1) / PT_BOX;
-        const int64_t segs = ((int64_t)a->n_rows * p.G / (16 * mt) + a->n_seqs) * p.Hk;
+        const int64_t segs = ((int64_t)a->n_rows * p.G / (16 * p.tiles) + a->n_seqs) * p.Hk;
         shares = (int)std::max<int64_t>(1, std::min<int64_t>(shares, segs * (boxes + PT_END_BOXES) / (PT_MIN_SHARE + PT_END_BOXES) + 1));
         if (boxes <= PT_WHOLE) {
             p.whole_boxes = INT_MAX;
             join = false;
         }
     }
-    const cudaError_t e = a->pool.head_dim == 64 ? launch_types<64>(a->pool.type, a->q_type, mt, p, mk, mv, shares, join, (cudaStream_t)cuda_stream)
-                                                 : launch_types<128>(a->pool.type, a->q_type, mt, p, mk, mv, shares, join, (cudaStream_t)cuda_stream);
+    const cudaError_t e = a->pool.head_dim == 64 ? launch_types<64>(a->pool.type, a->q_type, p, mk, mv, shares, join, (cudaStream_t)cuda_stream)
+                                                 : launch_types<128>(a->pool.type, a->q_type, p, mk, mv, shares, join, (cudaStream_t)cuda_stream);
     return e == cudaSuccess ? SPARSK_OK : SPARSK_ECUDA;
 }

@@ -2,7 +2,7 @@
 //
 //   out = sum_p w_p v_p / sum_p w_p,  w_p = exp(scale q.k_p - max), the maximum and both sums running (one pass).
 //
-// A segment is (sequence, block of 16 MT query vectors, kv head): the rows' query heads of that kv head are the M dimension of
+// A segment is (sequence, block of up to 64 query vectors, kv head): the rows' query heads of that kv head are the M dimension of
 // m16n8k16 products (as in sparsk_attn.cuh), so that one read of the head's keys and values serves all of them.
 // All segments, laid end to end in boxes of 16 positions (plus a few boxes' worth for a segment's set-up and end), are cut into equal
 // shares, one for each CTA of a grid that is resident at once: nobody knows the lengths but the device, and
@@ -12,9 +12,9 @@
 //
 // Within a CTA one warp brings boxes of 16 positions by TMA (a tensor map of the pool: dimensions, positions of a page, halves of
 // the head, heads, pages, whichever of heads and positions lies outside; a box never leaves its page, whose size is a multiple of 16) into
-// a ring of stages of 64 positions, and four warps take boxes from it: with MT = 1 a box each, with MT = 2 two boxes
-// each for one of two blocks of 16 query vectors, with MT = 4 all four for one of four.  Every warp keeps the softmax of
-// its own positions; the warps of one block meet at the segment's end only.  8-bit pages are widened to fp16 in
+// a ring of stages of 64 positions, and four warps take boxes from it: a box each where the segment has up to 16 query
+// vectors, two boxes each for one of two tiles of 16 where it has up to 32, else all four for one of four.  Every warp
+// keeps the softmax of its own positions; the warps of one tile meet at the segment's end only.  8-bit pages are widened to fp16 in
 // registers, between the shared memory and the product.
 // Bound by HBM: a position of a head of 128 fp16 numbers is 512 bytes, 23 of which come per clock and SM, so 16 positions
 // may take 350 clocks of an SM.
@@ -34,12 +34,13 @@ constexpr int PT_MAX_SHARES = 2 * 160;         // CTAs of a launch (the scratch 
 constexpr int PT_END_BOXES = 3;                // what a segment's set-up and end cost, in boxes
 constexpr int PT_WHOLE = 8;                    // a segment of up to so many boxes is never cut
 constexpr int PT_MIN_SHARE = 7;                // boxes
-constexpr int PT_RING_BYTES = 96 * 1024;
+constexpr float PT_LAG = 8.f;                  // in powers of two
+constexpr int PT_RING_BYTES = 112 * 1024;
 constexpr int PJ_THREADS = 256;
 
 // A share's partials for the join: bit 0 its last segment goes on in the next share, bits 1..2 its first one began in an
 // earlier share and 1 goes on, 2 ends here; and which segment the last one is.
-struct PtRecord {
+struct __align__(16) PtRecord {
     int flags, row0, rows, qblk, head, pad[3];
 };
 struct PtStage {  // what the computing warps have to know of a stage
@@ -56,12 +57,20 @@ struct PtArgs {
     const int *block_table, *seq_len, *row_start;
     const float *k_scale, *v_scale;
     PtRecord *records;  // [shares]
-    float4 *part_o;     // [shares][2][MT][HD / 8][32 lanes]: accumulators as the lanes hold them
-    float2 *part_ml;    // [shares][2][16 MT]: maximum in powers of two, sum
+    float4 *part_o;     // [shares][2][tiles][HD / 8][32 lanes]: accumulators as the lanes hold them
+    float2 *part_ml;    // [shares][2][tiles][16]: maximum in powers of two, sum
     long long table_stride, q_row_stride, q_head_stride, out_row_stride, out_head_stride;
     float scale_log2;
     int q_type, n_rows, n_seqs, max_blocks, page_size, n_pages, Hk, G;
+    int tiles;          // of 16 query vectors, in a segment at most (1, 2 or 4)
     int whole_boxes;    // segments of up to so many boxes are never cut
+    uint32_t g_inverse, g_limit;  // ceil(2^32 / G), and below which numbers it divides by G exactly
+    int q_words, out_words;  // queries and outputs may be read and written two numbers at a time
+};
+
+struct PtFirst {  // the sequence in which a share begins, and where its boxes do
+    long long at;
+    int seq, row0, rows, len;
 };
 
 template <int HD, int CT>
@@ -69,15 +78,18 @@ struct PtForm {
     static constexpr int ES = CT == SPARSK_E4M3 ? 1 : 2;
     static constexpr int RB = HD * ES;                          // bytes of a position
     static constexpr int STAGE = 2 * PT_STAGE * RB;             // keys, then values
-    static constexpr int NS = PT_RING_BYTES / STAGE;
-    static constexpr int MEET = PT_WARPS * (HD / 16) * 32 * 16; // the warps' sums, half of the dimensions at a time
-    static constexpr int SMEM = NS * STAGE + MEET + NS * (16 + (int)sizeof(PtStage)) + PT_WARPS * 16 * 8 + 80;
+    static constexpr int SUMS = PT_WARPS * (HD / 8) * 32 * 16;  // the warps' accumulators
+    static constexpr int MEET = SUMS > STAGE ? SUMS - STAGE : 0; // what of them a stage does not hold
+    static constexpr int FIT = (PT_RING_BYTES - MEET) / STAGE, NS = FIT < 12 ? FIT : 12;
+    static constexpr int SMEM = NS * STAGE + MEET + NS * (24 + (int)sizeof(PtStage)) + PT_WARPS * 16 * 8 + 40 + (int)sizeof(PtFirst) + 16;
     // byte offset of 16-byte chunk c of row r inside a box
     __device__ __forceinline__ static int at(int r, int c)
     {
         if (RB == 64) return r * 64 + ((c ^ ((r >> 1) & 3)) << 4);
         return (RB > 128 ? (c >> 3) * (PT_BOX * 128) : 0) + r * 128 + (((c & 7) ^ (r & 7)) << 4);
     }
+    // at(r, c0 + c) from at(r, c0), c0 below 2 and c even
+    __device__ __forceinline__ static int turn(int at0, int c) { return (at0 ^ ((c & 7) << 4)) + (c >> 3) * (PT_BOX * 128); }
 };
 
 __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *map, uint64_t *bar, int y, int head, int page)
@@ -108,9 +120,8 @@ __device__ __forceinline__ uint32_t pt_widen(uint32_t two)
 }
 // Two query numbers in the type that meets the pool's: a number beyond fp16 as its largest.
 template <int CT>
-__device__ __forceinline__ uint32_t pt_query2(const uint16_t *p, int q_type)
+__device__ __forceinline__ uint32_t pt_query2(uint32_t w, int q_type)
 {
-    const uint32_t w = (uint32_t)p[0] | ((uint32_t)p[1] << 16);
     if (CT == SPARSK_BF16 || q_type == SPARSK_FP16) return w;
     return pack_h2(pa_clamp_fp16(bf_lo(w)), pa_clamp_fp16(bf_hi(w)));
 }
@@ -156,32 +167,98 @@ __device__ __forceinline__ PtSeq pt_seq(const PtArgs &a, int i)
     s.len = max(__ldcg(a.seq_len + i), 0);  // as it was given; a table that ends earlier cuts it where it is used
     return s;
 }
-template <int MT>
-__device__ __forceinline__ int pt_blocks_of(const PtArgs &a, int rows) { return (int)(((long long)rows * a.G + 16 * MT - 1) / (16 * MT)); }
+// segments of a sequence
+__device__ __forceinline__ long long pt_segments(const PtArgs &a, int rows)
+{
+    const int shift = a.tiles == 1 ? 4 : a.tiles == 2 ? 5 : 6;
+    return (((long long)rows * a.G + (1 << shift) - 1) >> shift) * a.Hk;
+}
+// x / y for x >= 0, y > 0; almost always of 32 bits, which divide several times as fast
+__device__ __forceinline__ long long pt_div(long long x, int y)
+{
+    return (x >> 32) == 0 ? (long long)((unsigned)x / (unsigned)y) : x / y;
+}
+// v / G for a query vector's number
+__device__ __forceinline__ int pt_row_of(const PtArgs &a, int v)
+{
+    return (uint32_t)v < a.g_limit ? (int)__umulhi((uint32_t)v, a.g_inverse) : v / a.G;
+}
+// A wait that ends: the hardware's own, again and again until the phase is over, somebody has given up or two seconds have gone.
+__device__ __forceinline__ bool pt_wait(uint64_t *bar, uint32_t parity, volatile int *giving_up)
+{
+    const uint32_t at = smem_u32(bar);
+    unsigned long long t0 = 0;
+    for (uint32_t spin = 0;; spin++) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(at), "r"(parity)
+            : "memory");
+        if (__all_sync(0xffffffffu, ok)) return true;
+        if ((spin & 63u) == 63u) {
+            bool stop = *giving_up;
+            const unsigned long long now = global_ns();
+            if (t0 == 0) t0 = now;
+            else if (now - t0 > WAIT_TIMEOUT_NS) stop = true;
+            if (__any_sync(0xffffffffu, stop)) {
+                *giving_up = 1;
+                return false;
+            }
+        }
+    }
+}
 
-template <int HD, int CT, int MT, bool P2>
+// The outputs of one vector from two neighbouring products: two and two numbers side by side, or, where the products took
+// even and odd dimensions (8-bit pages), four.
+template <int ES>
+__device__ __forceinline__ void pt_put(const PtArgs &a, long long to, int nt, int t4, float e0, float e1, float o0, float o1)
+{
+    const auto two = [&](float x, float y) { return a.q_type == SPARSK_BF16 ? pack_bf16x2(x, y) : pack_h2(x, y); };
+    const uint32_t w0 = ES == 1 ? two(e0, o0) : two(e0, e1), w1 = ES == 1 ? two(e1, o1) : two(o0, o1);
+    uint16_t *p0 = reinterpret_cast<uint16_t *>(a.out) + to + nt * 8 + t4 * (ES == 1 ? 4 : 2), *p1 = p0 + (ES == 1 ? 2 : 8);
+    if (a.out_words) {
+        *reinterpret_cast<uint32_t *>(p0) = w0;
+        *reinterpret_cast<uint32_t *>(p1) = w1;
+    } else {
+        p0[0] = (uint16_t)w0;
+        p0[1] = (uint16_t)(w0 >> 16);
+        p1[0] = (uint16_t)w1;
+        p1[1] = (uint16_t)(w1 >> 16);
+    }
+}
+
+template <int HD, int CT, bool P2>
 static __global__ void __launch_bounds__(PT_THREADS, PT_CTAS)
 paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv)
 {
     typedef PtForm<HD, CT> F;
-    constexpr int NS = F::NS, RB = F::RB, KS = HD / 16, NT = HD / 8, PG = PT_WARPS / MT;
+    constexpr int NS = F::NS, RB = F::RB, KS = HD / 16, NT = HD / 8;
     constexpr float LN2 = 0.6931471805599453f;
     extern __shared__ __align__(1024) unsigned char pt_smem[];
     unsigned char *ring = pt_smem;
     float4 *meet = reinterpret_cast<float4 *>(pt_smem + NS * F::STAGE);
-    uint64_t *full = reinterpret_cast<uint64_t *>(pt_smem + NS * F::STAGE + F::MEET), *empty = full + NS;
-    PtStage *stages = reinterpret_cast<PtStage *>(empty + NS);
+    uint64_t *full = reinterpret_cast<uint64_t *>(pt_smem + NS * F::STAGE + F::MEET), *empty = full + NS, *told = empty + NS;
+    PtStage *stages = reinterpret_cast<PtStage *>(told + NS);
     float2 *meet_ml = reinterpret_cast<float2 *>(stages + NS);
-    long long *plan = reinterpret_cast<long long *>(meet_ml + PT_WARPS * 16);  // [5 sums of warps], first sequence and its begin
-    uint64_t *meeting = reinterpret_cast<uint64_t *>(plan + 7);
-    volatile int *giving_up = reinterpret_cast<volatile int *>(plan + 8);
+    long long *plan = reinterpret_cast<long long *>(meet_ml + PT_WARPS * 16);  // the warps' sums
+    PtFirst *first = reinterpret_cast<PtFirst *>(plan + PT_WARPS + 1);
+    uint64_t *meeting = reinterpret_cast<uint64_t *>(first + 1);
+    volatile int *giving_up = reinterpret_cast<volatile int *>(meeting + 1);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
     griddep_launch();
+    if (tid == 32) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&mk) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&mv) : "memory");
+    }
     if (tid == 0) {
         for (int s = 0; s < NS; s++) {
             mbar_init(&full[s], 1);
             mbar_init(&empty[s], PT_WARPS);
+            mbar_init(&told[s], 1);
         }
         mbar_init(meeting, PT_WARPS);
         giving_up[0] = giving_up[1] = 0;
@@ -194,9 +271,10 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
     const auto cost_of = [&](const PtSeq &s) { return (min(s.len, cap) + PT_BOX - 1) / PT_BOX + PT_END_BOXES; };
     const int per = (a.n_seqs + PT_THREADS - 1) / PT_THREADS, s_beg = min(tid * per, a.n_seqs), s_end = min(s_beg + per, a.n_seqs);
     long long mine = 0;
+    PtSeq s{};
     for (int i = s_beg; i < s_end; i++) {
-        const PtSeq s = pt_seq(a, i);
-        mine += (long long)pt_blocks_of<MT>(a, s.rows) * a.Hk * cost_of(s);
+        s = pt_seq(a, i);
+        mine += pt_segments(a, s.rows) * cost_of(s);
     }
     long long upto = mine;
 #pragma unroll
@@ -212,7 +290,7 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
         if (w < warp) upto += plan[w];
         total += plan[w];
     }
-    const long long share = max((total + gridDim.x - 1) / gridDim.x, (long long)(PT_MIN_SHARE + PT_END_BOXES));
+    const long long share = max(pt_div(total + gridDim.x - 1, gridDim.x), (long long)(PT_MIN_SHARE + PT_END_BOXES));
     const long long beg = share * blockIdx.x, end = min(beg + share, total);
     if (beg >= end) {
         if (tid == 0) a.records[blockIdx.x].flags = 0;
@@ -220,50 +298,50 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
     }
     if (mine > 0 && upto - mine <= beg && beg < upto) {  // the sequence in which it begins is one of this thread's
         long long at = upto - mine;
-        for (int i = s_beg; i < s_end; i++) {
-            const PtSeq s = pt_seq(a, i);
-            const long long c = (long long)pt_blocks_of<MT>(a, s.rows) * a.Hk * cost_of(s);
-            if (beg < at + c) {
-                plan[5] = i;
-                plan[6] = at;
-                break;
+        int i = s_beg;
+        if (per > 1)
+            for (;; i++) {
+                s = pt_seq(a, i);
+                const long long c = pt_segments(a, s.rows) * cost_of(s);
+                if (beg < at + c) break;
+                at += c;
             }
-            at += c;
-        }
+        *first = PtFirst{at, i, s.row0, s.rows, s.len};
     }
     __syncthreads();
 
     if (warp == PT_WARPS) {
         // ---------------------------------------------------------------- the warp that brings the boxes
-        int seq = (int)plan[5], base = -64, it = 0, issued = 0, flags = 0;
-        long long at = plan[6], x = beg;
+        int seq = first->seq, base = seq, it = 0, issued = 0, flags = 0;
+        long long at = first->at, x = beg;
+        PtSeq now{first->row0, first->rows, first->len};
         PtSeq ahead{};  // of sequence base + lane
+        if (seq + lane < a.n_seqs) ahead = pt_seq(a, seq + lane);
         PtRecord rec{};
         bool ok = true;
         const auto next_stage = [&]() {
             const int s = it % NS;
-            if (it >= NS) ok = __all_sync(0xffffffffu, mbar_wait(&empty[s], ((it / NS) - 1) & 1, giving_up, nullptr));
+            if (it >= NS) ok = pt_wait(&empty[s], ((it / NS) - 1) & 1, giving_up);
             it++;
             return s;
         };
         const int page_boxes = a.page_size / PT_BOX;
         while (ok && x < end) {
-            if (seq - base >= 32) {
-                base = seq;
-                if (seq + lane < a.n_seqs) ahead = pt_seq(a, seq + lane);
-            }
-            PtSeq s;
-            s.row0 = __shfl_sync(0xffffffffu, ahead.row0, seq - base);
-            s.rows = __shfl_sync(0xffffffffu, ahead.rows, seq - base);
-            s.len = __shfl_sync(0xffffffffu, ahead.len, seq - base);
-            const int cost = cost_of(s), boxes = cost - PT_END_BOXES;
-            const long long all = (long long)pt_blocks_of<MT>(a, s.rows) * a.Hk * cost;
+            const int cost = cost_of(now), boxes = cost - PT_END_BOXES;
+            const long long all = pt_segments(a, now.rows) * cost;
             if (x >= at + all) {
                 at += all;
                 seq++;
+                if (seq - base >= 32) {
+                    base = seq;
+                    if (seq + lane < a.n_seqs) ahead = pt_seq(a, seq + lane);
+                }
+                now.row0 = __shfl_sync(0xffffffffu, ahead.row0, seq - base);
+                now.rows = __shfl_sync(0xffffffffu, ahead.rows, seq - base);
+                now.len = __shfl_sync(0xffffffffu, ahead.len, seq - base);
                 continue;
             }
-            const long long seg = (x - at) / cost;
+            const long long seg = pt_div(x - at, cost);
             const int from = (int)(x - at - seg * cost);
             int to = (int)min((long long)cost, from + (end - x));
             x += to - from;
@@ -273,7 +351,7 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
             }
             const int b0 = min(from, boxes), b1 = min(to, boxes);
             if (b0 >= b1 && !(boxes == 0 && from == 0)) continue;
-            const int qblk = (int)(seg / a.Hk), head = (int)(seg % a.Hk);
+            const int qblk = (int)pt_div(seg, a.Hk), head = (int)(seg - (long long)qblk * a.Hk);
             int part = 0;
             if (b0 > 0) {
                 part = PT_HEAD_PART;
@@ -281,12 +359,19 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
             } else if (b1 < boxes) {
                 part = PT_TAIL_PART;
                 flags |= 1;
-                rec.row0 = s.row0;
-                rec.rows = s.rows;
+                rec.row0 = now.row0;
+                rec.rows = now.rows;
                 rec.qblk = qblk;
                 rec.head = head;
             }
-            const int pos_end = min(min(s.len, cap), b1 * PT_BOX);
+            // the queries on their way to the L2, behind which a whole stage's copies would have to wait
+            const int n_here = min(now.rows * a.G - qblk * a.tiles * 16, a.tiles * 16);
+            for (int i = lane; i < n_here * (HD / 64); i += 32) {
+                const int v = qblk * a.tiles * 16 + i / (HD / 64), r = pt_row_of(a, v);
+                prefetch_l2(reinterpret_cast<const uint16_t *>(a.q) + (now.row0 + r) * a.q_row_stride +
+                            (head * a.G + v - r * a.G) * a.q_head_stride + i % (HD / 64) * 64);
+            }
+            const int pos_end = min(min(now.len, cap), b1 * PT_BOX);
             int page = -1;
             for (int b = b0; ok && (b < b1 || b == b0); b += 4) {
                 const int chunk = (b - b0) & 31;
@@ -307,11 +392,12 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
                     d.end = pos_end;
                     d.flags = (b == b0 ? PT_FIRST : 0) | (b + 4 >= b1 ? PT_LAST : 0) | part |
                               ((have & 1u) << 8) | ((have & 4u) << 7) | ((have & 16u) << 6) | ((have & 64u) << 5);
-                    d.row0 = s.row0;
-                    d.rows = s.rows;
-                    d.len = s.len;
+                    d.row0 = now.row0;
+                    d.rows = now.rows;
+                    d.len = now.len;
                     d.qblk = qblk;
                     d.head = head;
+                    mbar_arrive(&told[st]);
                     mbar_expect_tx(&full[st], (uint32_t)__popc(have) * 2u * PT_BOX * RB);
                 }
                 __syncwarp();
@@ -327,6 +413,7 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
             const int st = next_stage();
             if (lane == 0 && ok) {
                 stages[st].flags = PT_STOP;
+                mbar_arrive(&told[st]);
                 mbar_arrive(&full[st]);
             }
         }
@@ -336,52 +423,78 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
         }
         // someone has given up: no copy may land in shared memory that is another CTA's by then
         if (!ok)
-            for (int k = max(0, issued - NS); k < issued; k++) mbar_wait(&full[k % NS], (k / NS) & 1, giving_up + 1, nullptr);
+            for (int k = max(0, issued - NS); k < issued; k++) pt_wait(&full[k % NS], (k / NS) & 1, giving_up + 1);
         return;
     }
 
     // -------------------------------------------------------------------- the warps that compute
-    const int mt = warp % MT, pg = warp / MT, t4 = lane & 3;
+    const int t4 = lane & 3;
+    int mt = 0, pg = 0, PG = 1;  // this warp's tile of 16 vectors, its place among the PG warps of the tile
     uint32_t qa[KS][4];
     float o[NT][4], m_run[2], l_run[2], c_log2 = 0.f;
+    // where this lane reads its rows of a box: the chunk's low bit is the lane's, even steps turn the others
+    const int k_at = F::at((lane & 7) + ((lane >> 4) << 3), (lane >> 3) & 1), v_at = F::at((lane & 7) + ((lane >> 3) & 1) * 8, lane >> 4);
     int limit[2], lim_min = 0, meetings = 0;
     // all four warps; like every wait here it ends by itself when another warp has given up
     const auto meet_here = [&]() {
         __syncwarp();
         if (lane == 0) mbar_arrive(meeting);
-        return __all_sync(0xffffffffu, mbar_wait(meeting, meetings++ & 1, giving_up, nullptr));
+        return pt_wait(meeting, meetings++ & 1, giving_up);
     };
     for (int it = 0;; it++) {
         const int st = it % NS;
-        if (!__all_sync(0xffffffffu, mbar_wait(&full[st], (it / NS) & 1, giving_up, nullptr))) return;
+        // what the stage holds is known before it has come: a new segment's queries are asked for meanwhile
+        if (!pt_wait(&told[st], (it / NS) & 1, giving_up)) return;
         const PtStage d = stages[st];
         if (d.flags & PT_STOP) break;
-        const int v0 = (d.qblk * MT + mt) * 16, n_vec = d.rows * a.G;  // this warp's query vectors: v0 .. v0 + 15, as far as there are
+        const int n_vec = d.rows * a.G;  // of the sequence
+        if (d.flags & PT_FIRST) {
+            const int n_here = min(n_vec - d.qblk * a.tiles * 16, a.tiles * 16), shift = n_here <= 16 ? 0 : n_here <= 32 ? 1 : 2;
+            mt = warp & ((1 << shift) - 1);
+            pg = warp >> shift;
+            PG = PT_WARPS >> shift;
+        }
+        const int v0 = (d.qblk * a.tiles + mt) * 16;  // this warp's query vectors: v0 .. v0 + 15, as far as there are
         if (d.flags & PT_FIRST) {
             c_log2 = a.scale_log2 * (a.k_scale ? a.k_scale[d.head] : 1.f);
 #pragma unroll
             for (int nt = 0; nt < NT; nt++)
 #pragma unroll
                 for (int e = 0; e < 4; e++) o[nt][e] = 0.f;
-            lim_min = d.len - d.rows + v0 / a.G;
+            lim_min = d.len - d.rows + pt_row_of(a, v0);
 #pragma unroll
             for (int hf = 0; hf < 2; hf++) {
                 const int v = v0 + (lane >> 2) + hf * 8;
                 const bool have = v < n_vec;
-                const int r = have ? v / a.G : 0, h = have ? v % a.G : 0;
+                const int r = have ? pt_row_of(a, v) : 0, h = have ? v - r * a.G : 0;
                 m_run[hf] = -INFINITY;
                 l_run[hf] = 0.f;
                 limit[hf] = have ? d.len - d.rows + r : -1;  // the last position that this vector sees
+                // (a tile's missing vectors compute with the sequence's first one, and nobody reads it)
                 const uint16_t *q = reinterpret_cast<const uint16_t *>(a.q) + (d.row0 + r) * a.q_row_stride + (d.head * a.G + h) * a.q_head_stride;
+                // 8-bit keys come four dimensions to a lane, 16-bit keys two and two
+                constexpr int STEP = F::ES == 1 ? 4 : 2, NEXT = F::ES == 1 ? 2 : 8;
+                if (a.q_words) {
 #pragma unroll
-                for (int ks = 0; ks < KS; ks++) {
-                    // 8-bit keys come four dimensions to a lane, 16-bit keys two and two
-                    const int d0 = ks * 16 + (F::ES == 1 ? t4 * 4 : t4 * 2), d1 = d0 + (F::ES == 1 ? 2 : 8);
-                    qa[ks][hf] = have ? pt_query2<CT>(q + d0, a.q_type) : 0u;
-                    qa[ks][2 + hf] = have ? pt_query2<CT>(q + d1, a.q_type) : 0u;
+                    for (int ks = 0; ks < KS; ks++) {
+                        qa[ks][hf] = *reinterpret_cast<const uint32_t *>(q + ks * 16 + t4 * STEP);
+                        qa[ks][2 + hf] = *reinterpret_cast<const uint32_t *>(q + ks * 16 + t4 * STEP + NEXT);
+                    }
+                } else {
+#pragma unroll
+                    for (int ks = 0; ks < KS; ks++) {
+                        const uint16_t *x = q + ks * 16 + t4 * STEP;
+                        qa[ks][hf] = (uint32_t)x[0] | ((uint32_t)x[1] << 16);
+                        qa[ks][2 + hf] = (uint32_t)x[NEXT] | ((uint32_t)x[NEXT + 1] << 16);
+                    }
                 }
             }
+#pragma unroll
+            for (int ks = 0; ks < KS; ks++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) qa[ks][i] = pt_query2<CT>(qa[ks][i], a.q_type);
         }
+        if (!pt_wait(&full[st], (it / NS) & 1, giving_up)) return;
         bool wrote = false;
 #pragma unroll 1
         for (int b = pg; b < 4; b += PG) {
@@ -394,13 +507,12 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
             for (int nt = 0; nt < 2; nt++)
 #pragma unroll
                 for (int e = 0; e < 4; e++) s[nt][e] = s2[nt][e] = 0.f;
-            const int krow = (lane & 7) + ((lane >> 4) << 3), kch = (lane >> 3) & 1;
             if constexpr (F::ES == 2) {
 #pragma unroll
                 for (int ks = 0; ks < KS; ks += 2) {
                     uint32_t kb[4], kb2[4];
-                    ldsm_x4(kb, K + F::at(krow, ks * 2 + kch));
-                    ldsm_x4(kb2, K + F::at(krow, (ks + 1) * 2 + kch));
+                    ldsm_x4(kb, K + F::turn(k_at, ks * 2));
+                    ldsm_x4(kb2, K + F::turn(k_at, ks * 2 + 2));
                     pt_mma<CT>(s[0], qa[ks], kb[0], kb[1]);
                     pt_mma<CT>(s[1], qa[ks], kb[2], kb[3]);
                     pt_mma<CT>(s2[0], qa[ks + 1], kb2[0], kb2[1]);
@@ -410,7 +522,7 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
 #pragma unroll
                 for (int ks = 0; ks < KS; ks += 2) {
                     uint32_t kb[4];
-                    ldsm_x4(kb, K + F::at(krow, ks + kch));
+                    ldsm_x4(kb, K + F::turn(k_at, ks));
                     pt_mma<CT>(s[0], qa[ks], pt_widen(kb[0]), pt_widen(kb[0] >> 16));
                     pt_mma<CT>(s2[0], qa[ks + 1], pt_widen(kb[1]), pt_widen(kb[1] >> 16));
                     pt_mma<CT>(s[1], qa[ks], pt_widen(kb[2]), pt_widen(kb[2] >> 16));
@@ -420,47 +532,55 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
             // a box that every vector sees whole needs no mask
             const bool whole = p0 + PT_BOX <= d.end && p0 + PT_BOX - 1 <= lim_min;
             uint32_t pa[4], pr[4];
-            float alpha[2];
+            float v[2][4], top[2];
+#pragma unroll
+            for (int hf = 0; hf < 2; hf++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) v[hf][i] = (s[i >> 1][hf * 2 + (i & 1)] + s2[i >> 1][hf * 2 + (i & 1)]) * c_log2;
+            if (!whole) {
+#pragma unroll
+                for (int hf = 0; hf < 2; hf++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const int p = p0 + (i >> 1) * 8 + t4 * 2 + (i & 1);
+                        if (p >= d.end || p > limit[hf]) v[hf][i] = -INFINITY;
+                    }
+            }
 #pragma unroll
             for (int hf = 0; hf < 2; hf++) {
-                float v[4], top = -INFINITY;
+                top[hf] = fmaxf(fmaxf(v[hf][0], v[hf][1]), fmaxf(v[hf][2], v[hf][3]));
+                top[hf] = fmaxf(top[hf], __shfl_xor_sync(0xffffffffu, top[hf], 1));
+                top[hf] = fmaxf(top[hf], __shfl_xor_sync(0xffffffffu, top[hf], 2));
+            }
+            // Weights are taken relative to a maximum that follows the true one only when that has grown by more than
+            // 2^PT_LAG: up to there they fit fp16 as well, and what was summed before needs no rescaling (which almost every box
+            // would ask for otherwise: it is enough that one of sixteen vectors meets a larger score).
+            if (__any_sync(0xffffffffu, top[0] > m_run[0] + PT_LAG || top[1] > m_run[1] + PT_LAG)) {
 #pragma unroll
-                for (int nt = 0; nt < 2; nt++)
+                for (int hf = 0; hf < 2; hf++) {
+                    const float m_new = top[hf] > m_run[hf] + PT_LAG ? top[hf] : m_run[hf];  // (each vector by its own scores alone)
+                    const float alpha = m_new == m_run[hf] ? 1.f : exp2f(m_run[hf] - m_new);  // 2^-inf = 0 at first
+                    m_run[hf] = m_new;
+                    l_run[hf] *= alpha;
 #pragma unroll
-                    for (int e = 0; e < 2; e++) {
-                        const int p = p0 + nt * 8 + t4 * 2 + e;
-                        const bool see = whole || (p < d.end && p <= limit[hf]);
-                        v[nt * 2 + e] = see ? (s[nt][hf * 2 + e] + s2[nt][hf * 2 + e]) * c_log2 : -INFINITY;
-                        top = fmaxf(top, v[nt * 2 + e]);
+                    for (int nt = 0; nt < NT; nt++) {
+                        o[nt][hf * 2] *= alpha;
+                        o[nt][hf * 2 + 1] *= alpha;
                     }
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                const float m_new = fmaxf(m_run[hf], top);
-                const float m_use = m_new == -INFINITY ? 0.f : m_new;  // nothing seen yet: every weight is 2^-inf = 0
-                alpha[hf] = exp2f(m_run[hf] - m_use);
-                if (m_run[hf] == m_new) alpha[hf] = 1.f;
-                float sum = 0.f;
-#pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    v[i] = exp2f(v[i] - m_use);
-                    sum += v[i];
-                }
-                l_run[hf] = l_run[hf] * alpha[hf] + sum;  // a lane's own positions; lanes are summed at the end
-                m_run[hf] = m_new;
-                pa[hf] = pt_pack2<CT>(v[0], v[1]);
-                pa[2 + hf] = pt_pack2<CT>(v[2], v[3]);
-                if (P2) {
-                    pr[hf] = pt_rest2<CT>(v[0], v[1], pa[hf]);
-                    pr[2 + hf] = pt_rest2<CT>(v[2], v[3], pa[2 + hf]);
                 }
             }
-            if (__any_sync(0xffffffffu, alpha[0] != 1.f || alpha[1] != 1.f)) {
 #pragma unroll
-                for (int nt = 0; nt < NT; nt++) {
-                    o[nt][0] *= alpha[0];
-                    o[nt][1] *= alpha[0];
-                    o[nt][2] *= alpha[1];
-                    o[nt][3] *= alpha[1];
+            for (int hf = 0; hf < 2; hf++) {
+                const float m = m_run[hf] == -INFINITY ? 0.f : m_run[hf];  // nothing seen yet: every weight is 2^-inf = 0
+                float w[4];
+#pragma unroll
+                for (int i = 0; i < 4; i++) w[i] = exp2f(v[hf][i] - m);
+                l_run[hf] += (w[0] + w[1]) + (w[2] + w[3]);  // a lane's own positions; lanes are summed at the end
+                pa[hf] = pt_pack2<CT>(w[0], w[1]);
+                pa[2 + hf] = pt_pack2<CT>(w[2], w[3]);
+                if (P2) {
+                    pr[hf] = pt_rest2<CT>(w[0], w[1], pa[hf]);
+                    pr[2 + hf] = pt_rest2<CT>(w[2], w[3], pa[2 + hf]);
                 }
             }
             // Values that nobody sees meet a weight of zero, which must not meet an infinity or a NaN: rows behind the end are
@@ -488,11 +608,10 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
                 odd_values = __any_sync(0xffffffffu, odd_values);  // (also: the cleared rows are written)
             }
             // O += P V
-            const int vrow = (lane & 7) + ((lane >> 3) & 1) * 8;
 #pragma unroll
             for (int np = 0; np < HD * F::ES / 32; np++) {
                 uint32_t vb[4], w[F::ES == 1 ? 8 : 4];
-                ldsm_x4_t(vb, V + F::at(vrow, np * 2 + (lane >> 4)));
+                ldsm_x4_t(vb, V + F::turn(v_at, np * 2));
                 constexpr int N = F::ES == 1 ? 4 : 2;  // products of eight dimensions each
                 if constexpr (F::ES == 1) {
                     // a word holds two positions of two dimensions: dimension by dimension
@@ -548,10 +667,15 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
                 }
             }
         }
+        const auto release = [&]() {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&empty[st]);
+        };
         if (wrote) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&empty[st]);
-        if (!(d.flags & PT_LAST)) continue;
+        if (!(d.flags & PT_LAST)) {
+            release();
+            continue;
+        }
 
         // ---------------------------------------------------------------- the piece's end
         float l[2], m[2] = {m_run[0], m_run[1]};
@@ -571,12 +695,10 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
 #pragma unroll
             for (int hf = 0; hf < 2; hf++) {
                 float top = -INFINITY, sum = 0.f;
-#pragma unroll
-                for (int g = 0; g < PG; g++) top = fmaxf(top, meet_ml[(g * MT + mt) * 16 + (lane >> 2) + hf * 8].x);
+                for (int g = 0; g < PG; g++) top = fmaxf(top, meet_ml[(warp + (g - pg) * (PT_WARPS / PG)) * 16 + (lane >> 2) + hf * 8].x);
                 const float use = top == -INFINITY ? 0.f : top;
-#pragma unroll
                 for (int g = 0; g < PG; g++) {
-                    const float2 x = meet_ml[(g * MT + mt) * 16 + (lane >> 2) + hf * 8];
+                    const float2 x = meet_ml[(warp + (g - pg) * (PT_WARPS / PG)) * 16 + (lane >> 2) + hf * 8];
                     sum += x.y * exp2f(x.x - use);
                 }
                 const float f = exp2f(m[hf] - use);
@@ -592,7 +714,7 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
             }
         }
         const bool part = d.flags & (PT_HEAD_PART | PT_TAIL_PART);
-        const size_t cell = ((size_t)blockIdx.x * 2 + (d.flags & PT_TAIL_PART ? 1 : 0)) * MT + mt;
+        const size_t cell = ((size_t)blockIdx.x * 2 + (d.flags & PT_TAIL_PART ? 1 : 0)) * a.tiles + mt;
         float inv[2];
         long long to[2];
         bool have[2];
@@ -601,7 +723,7 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
         for (int hf = 0; hf < 2; hf++) {
             const int v = v0 + (lane >> 2) + hf * 8;
             have[hf] = v < n_vec;
-            const int r = have[hf] ? v / a.G : 0, h = d.head * a.G + (have[hf] ? v % a.G : 0);
+            const int r = have[hf] ? pt_row_of(a, v) : 0, h = d.head * a.G + (have[hf] ? v - r * a.G : 0);
             to[hf] = (d.row0 + r) * a.out_row_stride + h * a.out_head_stride;
             inv[hf] = l[hf] == 0.f ? 0.f : __fdividef(vs, l[hf]);
             if (t4 == 0 && pg == 0) {
@@ -609,147 +731,139 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
                 else if (a.lse && have[hf]) a.lse[(long long)(d.row0 + r) * a.Hk * a.G + h] = l[hf] == 0.f ? -INFINITY : (m[hf] + log2f(l[hf])) * LN2;
             }
         }
-        const auto put = [&](int nt, const float4 &x) {
+        // Accumulators x0 and x1 of products nt and nt + 1, as a partial or as outputs.
+        const auto put = [&](int nt, const float4 &x0, const float4 &x1) {
             if (part) {
-                a.part_o[(cell * NT + nt) * 32 + lane] = x;
-                return;
+                a.part_o[(cell * NT + nt) * 32 + lane] = x0;
+                a.part_o[(cell * NT + nt + 1) * 32 + lane] = x1;
+            } else {
+                if (have[0]) pt_put<F::ES>(a, to[0], nt, t4, x0.x * inv[0], x0.y * inv[0], x1.x * inv[0], x1.y * inv[0]);
+                if (have[1]) pt_put<F::ES>(a, to[1], nt, t4, x0.z * inv[1], x0.w * inv[1], x1.z * inv[1], x1.w * inv[1]);
             }
-            const float y[4] = {x.x * inv[0], x.y * inv[0], x.z * inv[1], x.w * inv[1]};
-#pragma unroll
-            for (int hf = 0; hf < 2; hf++)
-                if (have[hf]) {
-#pragma unroll
-                    for (int e = 0; e < 2; e++) {
-                        const int dim = F::ES == 1 ? (nt >> 1) * 16 + t4 * 4 + e * 2 + (nt & 1) : nt * 8 + t4 * 2 + e;
-                        if (a.q_type == SPARSK_BF16) reinterpret_cast<bf16 *>(a.out)[to[hf] + dim] = __float2bfloat16(y[hf * 2 + e]);
-                        else reinterpret_cast<__half *>(a.out)[to[hf] + dim] = __float2half(y[hf * 2 + e]);
-                    }
-                }
         };
         if (PG == 1) {
+            release();
 #pragma unroll
-            for (int nt = 0; nt < NT; nt++) put(nt, make_float4(o[nt][0], o[nt][1], o[nt][2], o[nt][3]));
-        } else {
-#pragma unroll
-            for (int ph = 0; ph < 2; ph++) {  // half of the dimensions at a time
-#pragma unroll
-                for (int i = 0; i < NT / 2; i++)
-                    meet[(warp * (NT / 2) + i) * 32 + lane] =
-                        make_float4(o[ph * NT / 2 + i][0], o[ph * NT / 2 + i][1], o[ph * NT / 2 + i][2], o[ph * NT / 2 + i][3]);
-                if (!meet_here()) return;
-                for (int i = pg; i < NT / 2; i += PG) {
-                    float4 x = meet[(mt * (NT / 2) + i) * 32 + lane];
-#pragma unroll
-                    for (int g = 1; g < PG; g++) {
-                        const float4 y = meet[((g * MT + mt) * (NT / 2) + i) * 32 + lane];
-                        x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
-                    }
-                    put(ph * (NT / 2) + i, x);
-                }
-                if (!meet_here()) return;
-            }
+            for (int nt = 0; nt < NT; nt += 2)
+                put(nt, make_float4(o[nt][0], o[nt][1], o[nt][2], o[nt][3]), make_float4(o[nt + 1][0], o[nt + 1][1], o[nt + 1][2], o[nt + 1][3]));
+            continue;
         }
+        // the tile's warps add their sums up in the stage that they have just read (and held back)
+        const auto sums = [&](int w, int nt) {
+            const int i = (w * NT + nt) * 32 + lane;
+            return F::MEET && i >= F::STAGE / 16 ? meet + (i - F::STAGE / 16) : reinterpret_cast<float4 *>(ring + st * F::STAGE) + i;
+        };
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++) *sums(warp, nt) = make_float4(o[nt][0], o[nt][1], o[nt][2], o[nt][3]);
+        if (!meet_here()) return;
+#pragma unroll 1
+        for (int nt = pg * 2; nt < NT; nt += PG * 2) {
+            float4 x[2] = {*sums(mt, nt), *sums(mt, nt + 1)};
+#pragma unroll 1
+            for (int w = mt + PT_WARPS / PG; w < PT_WARPS; w += PT_WARPS / PG) {
+#pragma unroll
+                for (int k = 0; k < 2; k++) {
+                    const float4 y = *sums(w, nt + k);
+                    x[k].x += y.x; x[k].y += y.y; x[k].z += y.z; x[k].w += y.w;
+                }
+            }
+            put(nt, x[0], x[1]);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        release();
     }
 }
 
 // ------------------------------------------------------------------ the join
 // Share `blockIdx.x` ends in the middle of a segment: its last partial and the first ones of the shares behind it, up to
 // the one in which the segment ends.  blockIdx.y: which block of 16 vectors, and which quarter of the accumulators.
-template <int HD, int CT, int MT>
+template <int HD, int ES>
 static __global__ void __launch_bounds__(PJ_THREADS) paged_join_kernel(const PtArgs a, int shares)
 {
-    constexpr int NT = HD / 8, QN = NT / 4, COLS = QN * 32, GROUPS = PJ_THREADS / COLS;
+    // a block takes a quarter of a tile's accumulators: QP pairs of products, GROUPS partials side by side
+    constexpr int NT = HD / 8, QP = NT / 8, COLS = QP * 32, GROUPS = PJ_THREADS / COLS, PER = PJ_THREADS / 16;
     constexpr float LN2 = 0.6931471805599453f;
-    __shared__ float weight[PT_MAX_SHARES][16], red[PJ_THREADS / 16][16], sums[PJ_THREADS / 16][16];
-    __shared__ float4 acc[GROUPS][COLS];
-    __shared__ int count;
+    __shared__ float weight[PT_MAX_SHARES][16], red[PER][16], sums[PER][16];
+    __shared__ float4 acc[GROUPS][COLS][2];
+    const int w0 = blockIdx.x, mt = blockIdx.y >> 2, quarter = blockIdx.y & 3, tid = threadIdx.x, lane = tid & 31;
     griddep_wait();
-    const int w0 = blockIdx.x, mt = blockIdx.y >> 2, quarter = blockIdx.y & 3, tid = threadIdx.x;
-    PtRecord rec;
-    rec.flags = __ldcg(&a.records[w0].flags);
-    if (!(rec.flags & 1)) return;
-    rec.row0 = __ldcg(&a.records[w0].row0);
-    rec.rows = __ldcg(&a.records[w0].rows);
-    rec.qblk = __ldcg(&a.records[w0].qblk);
-    rec.head = __ldcg(&a.records[w0].head);
-    const int v0 = (rec.qblk * MT + mt) * 16, n_vec = rec.rows * a.G;
+    // the record, and where the segment ends: every warp for itself
+    const int4 rec = __ldcg(reinterpret_cast<const int4 *>(&a.records[w0]));
+    const int head = __ldcg(&a.records[w0].head);
+    int ends = w0 + 1 + lane < shares ? __ldcg(&a.records[w0 + 1 + lane].flags) & 4 : 0;
+    if (!(rec.x & 1)) return;
+    const int row0 = rec.y, v0 = (rec.w * a.tiles + mt) * 16, n_vec = rec.z * a.G;
     if (v0 >= n_vec) return;
-    if (tid < 32) {
-        int n = 1;
-        for (int w = w0 + 1; w < shares; w += 32) {
-            const bool last = w + tid < shares && (__ldcg(&a.records[w + tid].flags) & 4);
-            const uint32_t b = __ballot_sync(0xffffffffu, last);
-            if (b) {
-                n += __ffs(b);
-                break;
-            }
-            n += min(32, shares - w);
-        }
-        if (tid == 0) count = n;
+    int n = 1;
+    for (int w = w0 + 1;;) {
+        const uint32_t b = __ballot_sync(0xffffffffu, ends);
+        n += b ? __ffs(b) : min(32, shares - w);
+        w += 32;
+        if (b || w >= shares) break;
+        ends = w + lane < shares ? __ldcg(&a.records[w + lane].flags) & 4 : 0;
     }
-    __syncthreads();
-    const int n = count;
-    const auto cell = [&](int i) { return ((size_t)(w0 + i) * 2 + (i == 0 ? 1 : 0)) * MT + mt; };
+    const auto cell = [&](int i) { return ((size_t)(w0 + i) * 2 + (i == 0 ? 1 : 0)) * a.tiles + mt; };
     // weights of the partials for each vector
     const int v = tid & 15, i0 = tid >> 4;
     float top = -INFINITY;
-    for (int i = i0; i < n; i += PJ_THREADS / 16) {
-        const float2 x = __ldcg(&a.part_ml[cell(i) * 16 + v]);
-        weight[i][v] = x.x;
-        top = fmaxf(top, x.x);
+    for (int i = i0; i < n; i += PER) {
+        const float m = __ldcg(&a.part_ml[cell(i) * 16 + v]).x;
+        weight[i][v] = m;
+        top = fmaxf(top, m);
     }
     red[i0][v] = top;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < PJ_THREADS / 16; i++) top = fmaxf(top, red[i][v]);
+    for (int i = 0; i < PER; i++) top = fmaxf(top, red[i][v]);
     const float use = top == -INFINITY ? 0.f : top;
     float sum = 0.f;
-    for (int i = i0; i < n; i += PJ_THREADS / 16) {
+    for (int i = i0; i < n; i += PER) {
         const float f = exp2f(weight[i][v] - use);
         weight[i][v] = f;
         sum += f * __ldcg(&a.part_ml[cell(i) * 16 + v]).y;
     }
     sums[i0][v] = sum;
     __syncthreads();
-    const int col = tid % COLS, grp = tid / COLS, lane = col & 31, nt = quarter * QN + col / 32;
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int col = tid % COLS, grp = tid / COLS, nt = (quarter * QP + col / 32) * 2;
+    float4 x[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
 #pragma unroll 4
     for (int i = grp; i < n; i += GROUPS) {
-        const float4 y = __ldcg(&a.part_o[(cell(i) * NT + nt) * 32 + lane]);
         const float f0 = weight[i][lane >> 2], f1 = weight[i][(lane >> 2) + 8];
-        x.x += f0 * y.x; x.y += f0 * y.y; x.z += f1 * y.z; x.w += f1 * y.w;
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            const float4 y = __ldcg(&a.part_o[(cell(i) * NT + nt + k) * 32 + lane]);
+            x[k].x += f0 * y.x; x[k].y += f0 * y.y; x[k].z += f1 * y.z; x[k].w += f1 * y.w;
+        }
     }
-    acc[grp][col] = x;
+    acc[grp][col][0] = x[0];
+    acc[grp][col][1] = x[1];
     __syncthreads();
     if (grp > 0) return;
 #pragma unroll
-    for (int g = 1; g < GROUPS; g++) {
-        const float4 y = acc[g][col];
-        x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
-    }
-    const float vs = a.v_scale ? a.v_scale[rec.head] : 1.f;
-    const float val[4] = {x.x, x.y, x.z, x.w};
+    for (int g = 1; g < GROUPS; g++)
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            const float4 y = acc[g][col][k];
+            x[k].x += y.x; x[k].y += y.y; x[k].z += y.z; x[k].w += y.w;
+        }
+    const float vs = a.v_scale ? a.v_scale[head] : 1.f;
 #pragma unroll
     for (int hf = 0; hf < 2; hf++) {
         const int vec = (lane >> 2) + hf * 8;
         if (v0 + vec >= n_vec) continue;
         float l = 0.f;
 #pragma unroll
-        for (int i = 0; i < PJ_THREADS / 16; i++) l += sums[i][vec];
-        const int r = (v0 + vec) / a.G, h = rec.head * a.G + (v0 + vec) % a.G;
+        for (int i = 0; i < PER; i++) l += sums[i][vec];
+        const int r = pt_row_of(a, v0 + vec), h = head * a.G + v0 + vec - r * a.G;
         const float inv = l == 0.f ? 0.f : __fdividef(vs, l);
-#pragma unroll
-        for (int e = 0; e < 2; e++) {
-            const int dim = CT == SPARSK_E4M3 ? (nt >> 1) * 16 + (lane & 3) * 4 + e * 2 + (nt & 1) : nt * 8 + (lane & 3) * 2 + e;
-            const long long at = (rec.row0 + r) * a.out_row_stride + h * a.out_head_stride + dim;
-            if (a.q_type == SPARSK_BF16) reinterpret_cast<bf16 *>(a.out)[at] = __float2bfloat16(val[hf * 2 + e] * inv);
-            else reinterpret_cast<__half *>(a.out)[at] = __float2half(val[hf * 2 + e] * inv);
-        }
-        if (a.lse && quarter == 0 && nt == 0 && (lane & 3) == 0) {
+        const long long to = (row0 + r) * a.out_row_stride + h * a.out_head_stride;
+        if (hf == 0) pt_put<ES>(a, to, nt, lane & 3, x[0].x * inv, x[0].y * inv, x[1].x * inv, x[1].y * inv);
+        else pt_put<ES>(a, to, nt, lane & 3, x[0].z * inv, x[0].w * inv, x[1].z * inv, x[1].w * inv);
+        if (a.lse && nt == 0 && (lane & 3) == 0) {
             float m = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < PJ_THREADS / 16; i++) m = fmaxf(m, red[i][vec]);
-            a.lse[(long long)(rec.row0 + r) * a.Hk * a.G + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+            for (int i = 0; i < PER; i++) m = fmaxf(m, red[i][vec]);
+            a.lse[(long long)(row0 + r) * a.Hk * a.G + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
         }
     }
 }
