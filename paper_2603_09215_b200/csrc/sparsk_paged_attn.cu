@@ -175,7 +175,7 @@ extern "C" int sparsk_paged_attention(const sparsk_paged_attn_args *a, void *scr
         // the same, its share takes the whole of it)
         const int64_t boxes = ((int64_t)a->max_len + PT_BOX - 1) / PT_BOX;
         const int64_t segs = ((int64_t)a->n_rows * p.G / (16 * p.tiles) + a->n_seqs) * p.Hk;
-        shares = (int)std::max<int64_t>(1, std::min<int64_t>(shares, segs * (boxes + PT_END_BOXES) / (PT_MIN_SHARE + PT_END_BOXES) + 1));
+        shares = (int)std::max<int64_t>(1, std::min<int64_t>(shares, segs * (boxes * PT_C4 + PT_END_COST) / PT_MIN_SHARE + 1));
         if (boxes <= PT_WHOLE) {
             p.whole_boxes = INT_MAX;
             join = false;

@@ -27,13 +27,16 @@
 
 namespace sparsk {
 
-constexpr int PT_THREADS = 160, PT_WARPS = 4;  // four warps compute, the fifth brings the boxes
+constexpr int PT_THREADS = 256, PT_WARPS = 4;  // four warps compute, the fifth brings the boxes, three do nothing: registers
+// are given out by fours of warps, and the four that compute take most of what the others were launched with
+constexpr int PT_REGS = 200, PT_REGS_BRING = 56; // (times 128 threads each: the launch's 128 times 256)
 constexpr int PT_BOX = 16, PT_STAGE = 64;      // positions
 constexpr int PT_CTAS = 2;                     // resident on an SM
 constexpr int PT_MAX_SHARES = 2 * 160;         // CTAs of a launch (the scratch is sized for them)
-constexpr int PT_END_BOXES = 3;                // what a segment's set-up and end cost, in boxes
+constexpr int PT_END_COST = 24;                // a segment's set-up and end, in the unit of PtForm::box_cost
 constexpr int PT_WHOLE = 8;                    // a segment of up to so many boxes is never cut
-constexpr int PT_MIN_SHARE = 7;                // boxes
+constexpr int PT_MIN_SHARE = 28;               // the same unit
+constexpr int PT_C2 = 3, PT_C4 = 6;
 constexpr float PT_LAG = 8.f;                  // in powers of two
 constexpr int PT_RING_BYTES = 112 * 1024;
 constexpr int PJ_THREADS = 256;
@@ -81,7 +84,10 @@ struct PtForm {
     static constexpr int SUMS = PT_WARPS * (HD / 8) * 32 * 16;  // the warps' accumulators
     static constexpr int MEET = SUMS > STAGE ? SUMS - STAGE : 0; // what of them a stage does not hold
     static constexpr int FIT = (PT_RING_BYTES - MEET) / STAGE, NS = FIT < 12 ? FIT : 12;
-    static constexpr int SMEM = NS * STAGE + MEET + NS * (24 + (int)sizeof(PtStage)) + PT_WARPS * 16 * 8 + 40 + (int)sizeof(PtFirst) + 16;
+    static constexpr int SMEM = NS * STAGE + MEET + NS * (24 + (int)sizeof(PtStage)) + PT_WARPS * 16 * 8 + PT_THREADS / 4 + (int)sizeof(PtFirst) + 16;
+    // What a box costs where the segment has one tile of vectors (the stage's boxes go to four warps), two (two by two) or more
+    // (every box to every warp).
+    __host__ __device__ static constexpr int box_cost(int vectors) { return vectors <= 16 ? 2 : vectors <= 32 ? PT_C2 : PT_C4; }
     // byte offset of 16-byte chunk c of row r inside a box
     __device__ __forceinline__ static int at(int r, int c)
     {
@@ -151,6 +157,95 @@ __device__ __forceinline__ uint32_t pt_finite2(uint32_t w)
     if (pt_not_finite16<CT>(w & 0xffffu)) w &= 0xffff0000u;
     if (pt_not_finite16<CT>(w >> 16)) w &= 0xffffu;
     return w;
+}
+
+// Values that nobody sees meet a weight of zero, which must not meet an infinity or a NaN: the box's rows behind `end` are
+// cleared (`wrote`).  True (in all lanes) if rows that some vectors of a causal block see and others do not, those behind
+// lim_min, hold such numbers.
+template <int HD, int CT>
+__device__ __forceinline__ bool pt_clean(unsigned char *V, int p0, int end, int lim_min, int lane, bool &wrote)
+{
+    typedef PtForm<HD, CT> F;
+    constexpr int CH = F::RB / 16;
+    bool odd = false;
+#pragma unroll 1
+    for (int i = lane; i < PT_BOX * CH; i += 32) {
+        const int r = i / CH;
+        uint4 *w = reinterpret_cast<uint4 *>(V + F::at(r, i % CH));
+        if (p0 + r >= end) {
+            *w = make_uint4(0u, 0u, 0u, 0u);
+            wrote = true;
+        } else if (p0 + r > lim_min) {
+            const uint32_t x[4] = {w->x, w->y, w->z, w->w};
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                if (F::ES == 1) {
+#pragma unroll
+                    for (int y = 0; y < 4; y++) odd |= ((x[k] >> (8 * y)) & 0x7fu) == 0x7fu;
+                } else odd |= pt_not_finite16<CT>(x[k] & 0xffffu) || pt_not_finite16<CT>(x[k] >> 16);
+            }
+        }
+    }
+    return __any_sync(0xffffffffu, odd);  // (also: the cleared rows are written)
+}
+
+// O += P V for one box.  ODD: numbers that are not finite are left out of the products and given one by one to the vectors
+// that see them.
+template <int HD, int CT, bool P2, bool ODD>
+__device__ __forceinline__ void pt_values(float (&o)[HD / 8][4], const uint32_t (&pa)[4], const uint32_t (&pr)[4], const unsigned char *V,
+                                          int v_at, int lane, int p0, int end, const int (&limit)[2])
+{
+    typedef PtForm<HD, CT> F;
+    constexpr int N = F::ES == 1 ? 4 : 2;  // products of eight dimensions a load
+#pragma unroll
+    for (int np = 0; np < HD / 8 / N; np++) {
+        uint32_t vb[4], w[2 * N];
+        ldsm_x4_t(vb, V + F::turn(v_at, np * 2));
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            if constexpr (F::ES == 1) {
+                // a word holds two positions of two dimensions: dimension by dimension
+                const uint32_t x = __byte_perm(vb[i], 0, 0x3120);
+                w[(i >> 1) * 4 + (i & 1)] = pt_widen(x);
+                w[(i >> 1) * 4 + 2 + (i & 1)] = pt_widen(x >> 16);
+            } else w[i] = vb[i];
+        }
+        if (ODD) {
+#pragma unroll
+            for (int i = 0; i < 2 * N; i++) w[i] = pt_finite2<CT>(w[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            pt_mma<CT>(o[np * N + i], pa, w[2 * i], w[2 * i + 1]);
+            if (P2) pt_mma<CT>(o[np * N + i], pr, w[2 * i], w[2 * i + 1]);
+        }
+    }
+    if (!ODD) return;
+    const int t4 = lane & 3;
+#pragma unroll 1
+    for (int j = 0; j < PT_BOX && p0 + j < end; j++) {
+        const uint32_t w0 = __shfl_sync(0xffffffffu, j < 8 ? pa[0] : pa[2], (lane & ~3) + (j % 8) / 2);
+        const uint32_t w1 = __shfl_sync(0xffffffffu, j < 8 ? pa[1] : pa[3], (lane & ~3) + (j % 8) / 2);
+        float pj[2];
+#pragma unroll
+        for (int hf = 0; hf < 2; hf++) {
+            const uint32_t h = (hf ? w1 : w0) >> (16 * (j & 1)) & 0xffffu;
+            pj[hf] = CT == SPARSK_BF16 ? bf_lo(h) : __half2float(__ushort_as_half((unsigned short)h));
+        }
+#pragma unroll
+        for (int nt = 0; nt < HD / 8; nt++)
+#pragma unroll
+            for (int e = 0; e < 2; e++) {
+                const int dim = F::ES == 1 ? (nt >> 1) * 16 + t4 * 4 + e * 2 + (nt & 1) : nt * 8 + t4 * 2 + e;
+                const unsigned char *at_v = V + F::at(j, dim * F::ES / 16) + dim * F::ES % 16;
+                const uint32_t h = (F::ES == 1 ? pt_widen(*at_v) : *reinterpret_cast<const uint16_t *>(at_v)) & 0xffffu;
+                if (!pt_not_finite16<CT>(h)) continue;
+                const float f = CT == SPARSK_BF16 ? bf_lo(h) : __half2float(__ushort_as_half((unsigned short)h));
+#pragma unroll
+                for (int hf = 0; hf < 2; hf++)
+                    if (p0 + j <= limit[hf]) o[nt][hf * 2 + e] += pj[hf] * f;
+            }
+    }
 }
 
 // ------------------------------------------------------------------ the lengths, and a CTA's share of them
@@ -244,7 +339,7 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
     PtStage *stages = reinterpret_cast<PtStage *>(told + NS);
     float2 *meet_ml = reinterpret_cast<float2 *>(stages + NS);
     long long *plan = reinterpret_cast<long long *>(meet_ml + PT_WARPS * 16);  // the warps' sums
-    PtFirst *first = reinterpret_cast<PtFirst *>(plan + PT_WARPS + 1);
+    PtFirst *first = reinterpret_cast<PtFirst *>(plan + PT_THREADS / 32);
     uint64_t *meeting = reinterpret_cast<uint64_t *>(first + 1);
     volatile int *giving_up = reinterpret_cast<volatile int *>(meeting + 1);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -266,9 +361,19 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
     }
     griddep_wait();
 
+    // What the boxes' addresses and the queries wait for, on its way to the L2 while the lengths are added up: every CTA
+    // asks for its part of the tables (as far as that is a few lines a thread).
+    {
+        const int lines = (a.max_blocks + 31) / 32;
+        const long long all = (long long)lines * a.n_seqs, n_thr = (long long)gridDim.x * PT_THREADS;
+        if (all <= 4 * n_thr)
+            for (long long i = (long long)blockIdx.x * PT_THREADS + tid; i < all; i += n_thr) prefetch_l2(a.block_table + (i / lines) * a.table_stride + i % lines * 32);
+    }
     // this CTA's share [beg, end) of all segments' boxes
     const int cap = a.max_blocks * a.page_size;
-    const auto cost_of = [&](const PtSeq &s) { return (min(s.len, cap) + PT_BOX - 1) / PT_BOX + PT_END_BOXES; };
+    const auto boxes_of = [&](const PtSeq &s) { return (min(s.len, cap) + PT_BOX - 1) / PT_BOX; };
+    const auto box_cost = [&](const PtSeq &s) { return F::box_cost((int)min((long long)s.rows * a.G, a.tiles * 16LL)); };
+    const auto cost_of = [&](const PtSeq &s) { return boxes_of(s) * box_cost(s) + PT_END_COST; };
     const int per = (a.n_seqs + PT_THREADS - 1) / PT_THREADS, s_beg = min(tid * per, a.n_seqs), s_end = min(s_beg + per, a.n_seqs);
     long long mine = 0;
     PtSeq s{};
@@ -286,11 +391,11 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
     __syncthreads();
     long long total = 0;
 #pragma unroll
-    for (int w = 0; w < PT_WARPS + 1; w++) {
+    for (int w = 0; w < PT_THREADS / 32; w++) {
         if (w < warp) upto += plan[w];
         total += plan[w];
     }
-    const long long share = max(pt_div(total + gridDim.x - 1, gridDim.x), (long long)(PT_MIN_SHARE + PT_END_BOXES));
+    const long long share = max(pt_div(total + gridDim.x - 1, gridDim.x), (long long)PT_MIN_SHARE);
     const long long beg = share * blockIdx.x, end = min(beg + share, total);
     if (beg >= end) {
         if (tid == 0) a.records[blockIdx.x].flags = 0;
@@ -310,7 +415,9 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
     }
     __syncthreads();
 
-    if (warp == PT_WARPS) {
+    if (warp >= PT_WARPS) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PT_REGS_BRING));
+        if (warp > PT_WARPS) return;
         // ---------------------------------------------------------------- the warp that brings the boxes
         int seq = first->seq, base = seq, it = 0, issued = 0, flags = 0;
         long long at = first->at, x = beg;
@@ -327,7 +434,7 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
         };
         const int page_boxes = a.page_size / PT_BOX;
         while (ok && x < end) {
-            const int cost = cost_of(now), boxes = cost - PT_END_BOXES;
+            const int cost = cost_of(now), boxes = boxes_of(now), each = box_cost(now);
             const long long all = pt_segments(a, now.rows) * cost;
             if (x >= at + all) {
                 at += all;
@@ -349,7 +456,8 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
                 if (from > 0) continue;  // the share before this one has it
                 to = cost;
             }
-            const int b0 = min(from, boxes), b1 = min(to, boxes);
+            // a box is the share's in which its cost begins
+            const int b0 = min((from + each - 1) / each, boxes), b1 = min((to + each - 1) / each, boxes);
             if (b0 >= b1 && !(boxes == 0 && from == 0)) continue;
             const int qblk = (int)pt_div(seg, a.Hk), head = (int)(seg - (long long)qblk * a.Hk);
             int part = 0;
@@ -428,6 +536,7 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
     }
 
     // -------------------------------------------------------------------- the warps that compute
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(PT_REGS));
     const int t4 = lane & 3;
     int mt = 0, pg = 0, PG = 1;  // this warp's tile of 16 vectors, its place among the PG warps of the tile
     uint32_t qa[KS][4];
@@ -497,46 +606,40 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
         if (!pt_wait(&full[st], (it / NS) & 1, giving_up)) return;
         bool wrote = false;
 #pragma unroll 1
-        for (int b = pg; b < 4; b += PG) {
+        for (int b = v0 < n_vec ? pg : 4; b < 4; b += PG) {  // (a tile without vectors has nothing to do)
             const int p0 = d.p0 + b * PT_BOX;
             if (!(d.flags >> (8 + b) & 1)) continue;
             const unsigned char *K = ring + st * F::STAGE + b * (PT_BOX * RB), *V = K + PT_STAGE * RB;
             // S = Q K^T for 16 positions, two chains
-            float s[2][4], s2[2][4];
+            float s[2][2][4];
 #pragma unroll
-            for (int nt = 0; nt < 2; nt++)
+            for (int i = 0; i < 16; i++) s[i >> 3][i >> 2 & 1][i & 3] = 0.f;
 #pragma unroll
-                for (int e = 0; e < 4; e++) s[nt][e] = s2[nt][e] = 0.f;
-            if constexpr (F::ES == 2) {
-#pragma unroll
-                for (int ks = 0; ks < KS; ks += 2) {
-                    uint32_t kb[4], kb2[4];
+            for (int ks = 0; ks < KS; ks += 2) {
+                uint32_t kb[4];
+                if constexpr (F::ES == 2) {
+                    uint32_t kb2[4];
                     ldsm_x4(kb, K + F::turn(k_at, ks * 2));
                     ldsm_x4(kb2, K + F::turn(k_at, ks * 2 + 2));
-                    pt_mma<CT>(s[0], qa[ks], kb[0], kb[1]);
-                    pt_mma<CT>(s[1], qa[ks], kb[2], kb[3]);
-                    pt_mma<CT>(s2[0], qa[ks + 1], kb2[0], kb2[1]);
-                    pt_mma<CT>(s2[1], qa[ks + 1], kb2[2], kb2[3]);
-                }
-            } else {
-#pragma unroll
-                for (int ks = 0; ks < KS; ks += 2) {
-                    uint32_t kb[4];
+                    pt_mma<CT>(s[0][0], qa[ks], kb[0], kb[1]);
+                    pt_mma<CT>(s[0][1], qa[ks], kb[2], kb[3]);
+                    pt_mma<CT>(s[1][0], qa[ks + 1], kb2[0], kb2[1]);
+                    pt_mma<CT>(s[1][1], qa[ks + 1], kb2[2], kb2[3]);
+                } else {
                     ldsm_x4(kb, K + F::turn(k_at, ks));
-                    pt_mma<CT>(s[0], qa[ks], pt_widen(kb[0]), pt_widen(kb[0] >> 16));
-                    pt_mma<CT>(s2[0], qa[ks + 1], pt_widen(kb[1]), pt_widen(kb[1] >> 16));
-                    pt_mma<CT>(s[1], qa[ks], pt_widen(kb[2]), pt_widen(kb[2] >> 16));
-                    pt_mma<CT>(s2[1], qa[ks + 1], pt_widen(kb[3]), pt_widen(kb[3] >> 16));
+                    pt_mma<CT>(s[0][0], qa[ks], pt_widen(kb[0]), pt_widen(kb[0] >> 16));
+                    pt_mma<CT>(s[0][1], qa[ks], pt_widen(kb[2]), pt_widen(kb[2] >> 16));
+                    pt_mma<CT>(s[1][0], qa[ks + 1], pt_widen(kb[1]), pt_widen(kb[1] >> 16));
+                    pt_mma<CT>(s[1][1], qa[ks + 1], pt_widen(kb[3]), pt_widen(kb[3] >> 16));
                 }
             }
             // a box that every vector sees whole needs no mask
             const bool whole = p0 + PT_BOX <= d.end && p0 + PT_BOX - 1 <= lim_min;
-            uint32_t pa[4], pr[4];
             float v[2][4], top[2];
 #pragma unroll
             for (int hf = 0; hf < 2; hf++)
 #pragma unroll
-                for (int i = 0; i < 4; i++) v[hf][i] = (s[i >> 1][hf * 2 + (i & 1)] + s2[i >> 1][hf * 2 + (i & 1)]) * c_log2;
+                for (int i = 0; i < 4; i++) v[hf][i] = (s[0][i >> 1][hf * 2 + (i & 1)] + s[1][i >> 1][hf * 2 + (i & 1)]) * c_log2;
             if (!whole) {
 #pragma unroll
                 for (int hf = 0; hf < 2; hf++)
@@ -569,6 +672,7 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
                     }
                 }
             }
+            uint32_t pa[4], pr[4];
 #pragma unroll
             for (int hf = 0; hf < 2; hf++) {
                 const float m = m_run[hf] == -INFINITY ? 0.f : m_run[hf];  // nothing seen yet: every weight is 2^-inf = 0
@@ -583,89 +687,11 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
                     pr[2 + hf] = pt_rest2<CT>(w[2], w[3], pa[2 + hf]);
                 }
             }
-            // Values that nobody sees meet a weight of zero, which must not meet an infinity or a NaN: rows behind the end are
-            // cleared.  Rows that some vectors of a causal block see and others do not are looked at first.
-            bool odd_values = false;
-            if (!whole) {
-                constexpr int CH = RB / 16;
-                for (int i = lane; i < PT_BOX * CH; i += 32) {
-                    const int r = i / CH;
-                    uint4 *w = reinterpret_cast<uint4 *>(const_cast<unsigned char *>(V) + F::at(r, i % CH));
-                    if (p0 + r >= d.end) {
-                        *w = make_uint4(0u, 0u, 0u, 0u);
-                        wrote = true;
-                    } else if (p0 + r > lim_min) {
-                        const uint32_t x[4] = {w->x, w->y, w->z, w->w};
-#pragma unroll
-                        for (int k = 0; k < 4; k++) {
-                            if (F::ES == 1) {
-#pragma unroll
-                                for (int y = 0; y < 4; y++) odd_values |= ((x[k] >> (8 * y)) & 0x7fu) == 0x7fu;
-                            } else odd_values |= pt_not_finite16<CT>(x[k] & 0xffffu) || pt_not_finite16<CT>(x[k] >> 16);
-                        }
-                    }
-                }
-                odd_values = __any_sync(0xffffffffu, odd_values);  // (also: the cleared rows are written)
-            }
             // O += P V
-#pragma unroll
-            for (int np = 0; np < HD * F::ES / 32; np++) {
-                uint32_t vb[4], w[F::ES == 1 ? 8 : 4];
-                ldsm_x4_t(vb, V + F::turn(v_at, np * 2));
-                constexpr int N = F::ES == 1 ? 4 : 2;  // products of eight dimensions each
-                if constexpr (F::ES == 1) {
-                    // a word holds two positions of two dimensions: dimension by dimension
-#pragma unroll
-                    for (int i = 0; i < 4; i++) {
-                        const uint32_t x = __byte_perm(vb[i], 0, 0x3120);
-                        w[(i >> 1) * 4 + (i & 1)] = pt_widen(x);
-                        w[(i >> 1) * 4 + 2 + (i & 1)] = pt_widen(x >> 16);
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; i++) w[i] = vb[i];
-                }
-                if (odd_values) {
-#pragma unroll
-                    for (int i = 0; i < 2 * N; i++) w[i] = pt_finite2<CT>(w[i]);
-                }
-#pragma unroll
-                for (int i = 0; i < N; i++) {
-                    pt_mma<CT>(o[np * N + i], pa, w[2 * i], w[2 * i + 1]);
-                    if (P2) pt_mma<CT>(o[np * N + i], pr, w[2 * i], w[2 * i + 1]);
-                }
-            }
-            if (odd_values) {
-                // the numbers left out above, one by one, to the vectors that see them
-#pragma unroll 1
-                for (int j = 0; j < PT_BOX; j++) {
-                    const uint32_t w0 = __shfl_sync(0xffffffffu, j < 8 ? pa[0] : pa[2], (lane & ~3) + (j % 8) / 2);
-                    const uint32_t w1 = __shfl_sync(0xffffffffu, j < 8 ? pa[1] : pa[3], (lane & ~3) + (j % 8) / 2);
-                    float pj[2];
-#pragma unroll
-                    for (int hf = 0; hf < 2; hf++) {
-                        const uint32_t h = (hf ? w1 : w0) >> (16 * (j & 1)) & 0xffffu;
-                        pj[hf] = CT == SPARSK_BF16 ? bf_lo(h) : __half2float(__ushort_as_half((unsigned short)h));
-                    }
-                    if (p0 + j >= d.end) break;
-#pragma unroll
-                    for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                        for (int e = 0; e < 2; e++) {
-                            const int dim = F::ES == 1 ? (nt >> 1) * 16 + t4 * 4 + e * 2 + (nt & 1) : nt * 8 + t4 * 2 + e;
-                            const unsigned char *at_v = V + F::at(j, dim * F::ES / 16) + dim * F::ES % 16;
-                            uint32_t h;
-                            if (F::ES == 1) h = pt_widen(*at_v);
-                            else h = *reinterpret_cast<const uint16_t *>(at_v);
-                            h &= 0xffffu;
-                            if (!pt_not_finite16<CT>(h)) continue;
-                            const float f = CT == SPARSK_BF16 ? bf_lo(h) : __half2float(__ushort_as_half((unsigned short)h));
-#pragma unroll
-                            for (int hf = 0; hf < 2; hf++)
-                                if (p0 + j <= limit[hf]) o[nt][hf * 2 + e] += pj[hf] * f;
-                        }
-                }
-            }
+            bool odd = false;
+            if (!whole) odd = pt_clean<HD, CT>(const_cast<unsigned char *>(V), p0, d.end, lim_min, lane, wrote);
+            if (__builtin_expect(odd, 0)) pt_values<HD, CT, P2, true>(o, pa, pr, V, v_at, lane, p0, d.end, limit);
+            else pt_values<HD, CT, P2, false>(o, pa, pr, V, v_at, lane, p0, d.end, limit);
         }
         const auto release = [&]() {
             __syncwarp();
@@ -826,7 +852,7 @@ static __global__ void __launch_bounds__(PJ_THREADS) paged_join_kernel(const PtA
     __syncthreads();
     const int col = tid % COLS, grp = tid / COLS, nt = (quarter * QP + col / 32) * 2;
     float4 x[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-#pragma unroll 4
+#pragma unroll 8
     for (int i = grp; i < n; i += GROUPS) {
         const float f0 = weight[i][lane >> 2], f1 = weight[i][(lane >> 2) + 8];
 #pragma unroll
