@@ -1,16 +1,36 @@
 // A token for each row of logits by the row's own temperature, top-k, top-p and min-p.
+//
+// With w = exp((z - max) / T), the ids in the order of falling z (equal z: lower id first): every cut, and the draw, is the
+// question up to which id of that order a count or a mass reaches a target, and no sort is needed to answer it.
+//   1. Bins of equal width in (max - z) / T, as many as the row's range asks for (40 at most: beyond that even a
+//      quarter of a million ids weigh less than 2^-40 of the whole).  A bin adds up how many ids it holds and what they weigh; the sums of
+//      bins, in order, say in which bin a target lies.
+//   2. The bin's ids (some hundred, rarely) are gathered, ranked by counting and added up one by one.  A bin of more ids is
+//      divided again, by the bits of its logits, until few are left or all are equal.
+// Sums do not depend on the order of the additions: all masses are whole numbers of 2^-44, and within a bin the weights
+// are added as whole numbers too.  With x = s (max - z) / T, bin
+// b = floor(x) and f = x - b, an id weighs e^(-b/s) (1 - h / s), h = s (1 - e^(-f/s)) < 1, and h is added as a number of 32 bits behind
+// the point (s is 51 or more: 2^-38 of the id's weight).  x is worked out in 64 bits, h by five terms of its series
+// (the next one is 2^-38): a draw is decided at the border between two ids, and of a flat row of 150,000 ids each weighs 2^-17, so
+// that 24 bits would draw a neighbour once in a hundred times.  The FP64 units run at half the FP32 rate here.
+//
+// A row is read from memory once, into the shared memory of a cluster of up to eight CTAs.  Counts of a bin and the carries of its
+// h are the halves of one word, so an id costs two shared-memory atomics, which with the eight FP64 operations are what
+// bounds the kernel where there are many rows; five cluster barriers bound it where there is one.
 #pragma once
+
+#include <cooperative_groups.h>
 
 #include "../../include/sparsk.h"
 #include "sparsk_common.cuh"
 
 namespace sparsk {
 
-// A logit as an unsigned number of the same order; 0 for what can never be drawn (minus infinity, NaN).  The
-// two zeros are one number.
+namespace cg = cooperative_groups;
+
+// A logit as an unsigned number of the same order; 0 for what can never be drawn (minus infinity, NaN).
 __device__ __forceinline__ uint32_t st_key(uint32_t bits)
 {
-    if ((bits << 1) == 0u) return 0x80000000u;
     if ((bits << 1) > 0xff000000u || bits == 0xff800000u) return 0u;
     return (bits & 0x80000000u) ? ~bits : (bits | 0x80000000u);
 }
@@ -18,169 +38,596 @@ __device__ __forceinline__ uint32_t st_bits(uint32_t key) { return (key & 0x8000
 template <int TYPE>
 __device__ __forceinline__ uint32_t st_load(const void *p, long long at)
 {
-    if (TYPE == SPARSK_FP32) return reinterpret_cast<const uint32_t *>(p)[at];
-    const uint16_t h = reinterpret_cast<const uint16_t *>(p)[at];
-    if (TYPE == SPARSK_BF16) return (uint32_t)h << 16;
-    return __float_as_uint(__half2float(__ushort_as_half(h)));
+    uint32_t bits;
+    if (TYPE == SPARSK_FP32) bits = reinterpret_cast<const uint32_t *>(p)[at];
+    else {
+        const uint16_t h = reinterpret_cast<const uint16_t *>(p)[at];
+        bits = TYPE == SPARSK_BF16 ? (uint32_t)h << 16 : __float_as_uint(__half2float(__ushort_as_half(h)));
+    }
+    return (bits << 1) == 0u ? 0u : bits;  // the two zeros are one number
+}
+// The number as a double, by its bits (the conversion instruction runs at a quarter of the rate): infinity becomes 2^128,
+// zero 2^-127, which is all the same to the weights.
+__device__ __forceinline__ double st_double(uint32_t bits)
+{
+    return __hiloint2double((int)((bits & 0x80000000u) | (((bits & 0x7fffffffu) >> 3) + 0x38000000u)), (int)(bits << 29));
 }
 
-constexpr int ST_SIMPLE_THREADS = 1024;
+constexpr int ST_THREADS = 512, ST_WARPS = ST_THREADS / 32;
+constexpr int ST_BINS = 2048;   // the last one holds what lies beyond the range
+constexpr int ST_FEW = 512;     // ids that are ranked by counting
+constexpr double ST_RANGE = 40;
+constexpr double ST_UNIT = 17592186044416.0;  // 2^44 units of mass are the largest weight (2^18 ids of it fit 64 bits)
+constexpr uint32_t ST_DEAD = 0xffffffffu;
+constexpr double ST_POINT = 1048576.0;  // 2^20: a double from there on has 32 bits behind the point in its lower word
+constexpr uint32_t ST_POINT_HI = 0x41300000u;
 
-// One block a row; every question ("how many ids, and what mass, lie at or above this key") is a pass over the row.
-template <int TYPE>
-static __global__ void __launch_bounds__(ST_SIMPLE_THREADS) sample_simple_kernel(sparsk_sample_args a)
+enum { ST_BY_COUNT = 0, ST_BY_MASS = 1, ST_BEYOND = 2 };  // the first id at which the count, the mass reaches the target; the mass exceeds it
+
+struct StShared {
+    unsigned long long list[2][ST_FEW];  // gathered ids of this CTA, two lists in turn (the cluster reads them)
+    int list_n[2];
+    uint32_t pub_max[2], pub_min[2];     // this CTA's, for the cluster
+    unsigned long long pub_mass[2];
+    int pub_count[2];
+    // this CTA's own
+    unsigned long long all_mass[9];      // sums before each CTA of the cluster
+    int all_count[9];
+    unsigned long long wsum[ST_WARPS];
+    int wcnt[ST_WARPS];
+    uint32_t wmax[ST_WARPS], wmin[ST_WARPS];
+    int found, found_cnt, found_n;       // a search's answer: which, ids before it, ids in it
+    unsigned long long found_mass;       // mass before it
+    int taken;
+    unsigned long long taken_mass;
+};
+
+template <int C>
+struct StCluster {
+    __device__ __forceinline__ static int rank() { return C > 1 ? (int)cluster_rank() : 0; }
+    __device__ __forceinline__ static void sync()
+    {
+        if (C > 1) cluster_barrier();
+        else __syncthreads();
+    }
+    template <class T>
+    __device__ __forceinline__ static T *of(T *p, int r)
+    {
+        if (C > 1) return cg::this_cluster().map_shared_rank(p, r);
+        return p;
+    }
+};
+
+// Bins' sums: a bin's h in 32 bits and, in the other word, its ids (upper half) and the carries (lower half).
+__device__ __forceinline__ void st_add(uint32_t *lo, uint32_t *hi, int b, uint32_t h)
 {
-    __shared__ double wd[32];
-    __shared__ int wi[32];
-    __shared__ uint32_t wu[32];
-    const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t old = atomicAdd(lo + b, h);
+    atomicAdd(hi + b, 0x10000u + (old + h < old ? 1u : 0u));
+}
+
+template <int TYPE, int C>
+static __global__ void __launch_bounds__(ST_THREADS) settings_sample_kernel(sparsk_sample_args a)
+{
+    typedef StCluster<C> Cl;
+    constexpr int OWN = ST_BINS / C, PER = OWN > ST_THREADS ? OWN / ST_THREADS : 1;  // bins a CTA, a thread adds up
+    extern __shared__ __align__(16) unsigned char st_smem[];
+    uint32_t *bin_lo = reinterpret_cast<uint32_t *>(st_smem), *bin_hi = bin_lo + ST_BINS;
+    // ranked ids and their masses take the bins' place when these have been added up
+    unsigned long long *ranked = reinterpret_cast<unsigned long long *>(st_smem);
+    unsigned long long *ranked_mass = reinterpret_cast<unsigned long long *>(st_smem + ST_FEW * 8);
+    unsigned long long *own_mass = reinterpret_cast<unsigned long long *>(st_smem + ST_BINS * 8);  // before each of this CTA's bins
+    int *own_count = reinterpret_cast<int *>(own_mass + OWN);
+    uint32_t *slice = reinterpret_cast<uint32_t *>(own_count + OWN);
+    __shared__ StShared sh;
+    const int row = blockIdx.x / C, rank = Cl::rank(), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int lo = a.id_lo ? max(a.id_lo[row], 0) : 0, hi = a.id_hi ? min(a.id_hi[row], a.n_ids) : a.n_ids;
-    const long long base = row * a.row_stride;
-    uint32_t top = 0;
-    for (int i = lo + tid; i < hi; i += ST_SIMPLE_THREADS) top = max(top, st_key(st_load<TYPE>(a.logits, base + i)));
-    top = __reduce_max_sync(0xffffffffu, top);
-    if (lane == 0) wu[warp] = top;
-    __syncthreads();
-    for (int w = 0; w < 32; w++) top = max(top, wu[w]);
-    if (top == 0) {
-        if (tid == 0) {
+    const int n = max(hi - lo, 0), per_cta = (n + C - 1) / C, beg = min(rank * per_cta, n), mine = min(per_cta, n - beg);
+
+    // ---- the row, its largest and smallest logit
+    for (int b = tid; b < 2 * ST_BINS; b += ST_THREADS) bin_lo[b] = 0u;
+    uint32_t kmax = 0u, kmin = ~0u;
+    {
+        const long long at = row * a.row_stride + lo + beg;
+#pragma unroll 8
+        for (int i = tid; i < mine; i += ST_THREADS) {
+            const uint32_t bits = st_load<TYPE>(a.logits, at + i), k = st_key(bits);
+            slice[i] = k ? bits : ST_DEAD;
+            kmax = max(kmax, k);
+            kmin = min(kmin, k ? k : ~0u);
+        }
+    }
+    int turn = 0;  // of what the cluster reads: written anew two turns later, when everybody has passed the barrier between
+    const auto max_min = [&]() {
+        kmax = __reduce_max_sync(0xffffffffu, kmax);
+        kmin = __reduce_min_sync(0xffffffffu, kmin);
+        if (lane == 0) {
+            sh.wmax[warp] = kmax;
+            sh.wmin[warp] = kmin;
+        }
+        __syncthreads();
+        if (warp == 0) {
+            kmax = __reduce_max_sync(0xffffffffu, lane < ST_WARPS ? sh.wmax[lane] : 0u);
+            kmin = __reduce_min_sync(0xffffffffu, lane < ST_WARPS ? sh.wmin[lane] : ~0u);
+            if (lane == 0) {
+                sh.pub_max[turn] = kmax;
+                sh.pub_min[turn] = kmin;
+            }
+        }
+        Cl::sync();
+        kmax = 0u;
+        kmin = ~0u;
+#pragma unroll
+        for (int r = 0; r < C; r++) {
+            kmax = max(kmax, *Cl::of(&sh.pub_max[turn], r));
+            kmin = min(kmin, *Cl::of(&sh.pub_min[turn], r));
+        }
+        turn ^= 1;
+    };
+    max_min();
+    const uint32_t top = kmax;
+    if (top == 0u) {
+        if (rank == 0 && tid == 0) {
             a.token[row] = -1;
             if (a.logprob) a.logprob[row] = -INFINITY;
         }
+        Cl::sync();  // nobody leaves while its shared memory may be read
         return;
     }
     const float temp = a.temperature ? a.temperature[row] : 1.f;
     const bool greedy = !(temp > 0.f);
-    const double inv_t = greedy ? 1.0 : 1.0 / (double)temp, z0 = (double)__uint_as_float(st_bits(top));
-    const auto weight = [&](uint32_t key) { return key == top ? 1.0 : exp(((double)__uint_as_float(st_bits(key)) - z0) * inv_t); };
-    const auto ask = [&](uint32_t t, int &count, double &mass) {
-        int c = 0;
-        double m = 0;
-        for (int i = lo + tid; i < hi; i += ST_SIMPLE_THREADS) {
-            const uint32_t k = st_key(st_load<TYPE>(a.logits, base + i));
-            if (k != 0 && k >= t) {
-                c++;
-                m += weight(k);
+    const double z0 = st_double(st_bits(top)), inv_t = greedy ? 1.0 : 1.0 / (double)temp;
+    const double range = fmin((z0 - st_double(st_bits(kmin))) * inv_t, ST_RANGE);
+    const double s = range > 0 ? (ST_BINS - 1.001) / range : 1.0, scale = s * inv_t;
+    const double c1 = 0.5 / s, c2 = c1 / (3 * s), c3 = c2 / (4 * s), c4 = c3 / (5 * s);
+
+    // x of a logit, in ST_POINT's form
+    const auto place = [&](uint32_t bits) { return fma(z0 - st_double(bits), scale, ST_POINT); };
+    const auto bin_of = [&](double y) { return (int)min((uint32_t)__double2hiint(y) - ST_POINT_HI, (uint32_t)ST_BINS - 1u); };
+    const auto h_of = [&](double y) {
+        const double f = y - __hiloint2double(__double2hiint(y), 0);
+        return (uint32_t)__double2loint(fma(f, fma(-f, fma(-f, fma(-f, fma(-f, c4, c3), c2), c1), 1.0), ST_POINT));
+    };
+    const auto log_weight = [&](uint32_t key) { return key == top ? 0.0 : (st_double(st_bits(key)) - z0) * inv_t; };
+    const auto mass_of = [&](uint32_t key) { return __double2ull_rn(exp(log_weight(key)) * ST_UNIT); };
+
+    // ---- the bins
+    // Adds the ids for which `which` names a bin into them.  Warps whose ids all fall into one bin add up first.
+    const auto fill = [&](auto which) {
+#pragma unroll 4
+        for (int i0 = warp * 32; i0 < mine; i0 += ST_THREADS) {
+            const int i = i0 + lane;
+            const uint32_t bits = i < mine ? slice[i] : ST_DEAD;
+            const double y = place(bits);
+            const int b = bits == ST_DEAD ? -1 : which(bits, y);
+            const uint32_t h = bin_of(y) == ST_BINS - 1 ? 0u : h_of(y);
+            const int b0 = __shfl_sync(0xffffffffu, b, 0);
+            if (b0 >= 0 && __all_sync(0xffffffffu, b == b0)) {
+                const uint32_t h_lo = __reduce_add_sync(0xffffffffu, h & 0xffffu), h_hi = __reduce_add_sync(0xffffffffu, h >> 16);
+                if (lane == 0) {
+                    const unsigned long long all = ((unsigned long long)h_hi << 16) + h_lo;
+                    const uint32_t part = (uint32_t)all, old = atomicAdd(bin_lo + b, part);
+                    atomicAdd(bin_hi + b, (32u << 16) + (uint32_t)(all >> 32) + (old + part < old ? 1u : 0u));
+                }
+            } else if (b >= 0) st_add(bin_lo, bin_hi, b, h);
+        }
+    };
+    // The cluster's bins added up, this CTA's share of them: ids and mass before each; `e` of a bin is what its ids weigh less h / s.
+    const auto add_up = [&](auto e) {
+        Cl::sync();
+        int cnt[PER], c_sum = 0;
+        unsigned long long mass[PER], m_sum = 0;
+#pragma unroll
+        for (int k = 0; k < PER; k++) {
+            const int own = tid * PER + k, b = rank * OWN + own;
+            cnt[k] = 0;
+            mass[k] = 0;
+            if (own < OWN) {
+                unsigned long long h = 0;
+#pragma unroll
+                for (int r = 0; r < C; r++) {
+                    const uint32_t w = *Cl::of(bin_hi + b, r);
+                    cnt[k] += (int)(w >> 16);
+                    h += ((unsigned long long)(w & 0xffffu) << 32) + *Cl::of(bin_lo + b, r);
+                }
+                if (cnt[k]) mass[k] = __double2ull_rn(e(b) * ST_UNIT * ((double)cnt[k] - (double)h * (1.0 / 4294967296.0) / s));
+            }
+            c_sum += cnt[k];
+            m_sum += mass[k];
+        }
+        int c_in = c_sum;
+        unsigned long long m_in = m_sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int c = __shfl_up_sync(0xffffffffu, c_in, o);
+            const unsigned long long m = __shfl_up_sync(0xffffffffu, m_in, o);
+            if (lane >= o) {
+                c_in += c;
+                m_in += m;
             }
         }
-        for (int o = 16; o > 0; o >>= 1) {
-            c += __shfl_xor_sync(0xffffffffu, c, o);
-            m += __shfl_xor_sync(0xffffffffu, m, o);
+        if (lane == 31) {
+            sh.wcnt[warp] = c_in;
+            sh.wsum[warp] = m_in;
         }
         __syncthreads();
-        if (lane == 0) {
-            wi[warp] = c;
-            wd[warp] = m;
+        int c_at = 0, c_all = 0;
+        unsigned long long m_at = 0, m_all = 0;
+#pragma unroll
+        for (int w = 0; w < ST_WARPS; w++) {
+            if (w == warp) {
+                c_at = c_all;
+                m_at = m_all;
+            }
+            c_all += sh.wcnt[w];
+            m_all += sh.wsum[w];
         }
-        __syncthreads();
-        count = 0;
-        mass = 0;
-        for (int w = 0; w < 32; w++) {
-            count += wi[w];
-            mass += wd[w];
+        c_at += c_in - c_sum;
+        m_at += m_in - m_sum;
+#pragma unroll
+        for (int k = 0; k < PER; k++) {
+            if (tid * PER + k < OWN) {
+                own_count[tid * PER + k] = c_at;
+                own_mass[tid * PER + k] = m_at;
+            }
+            c_at += cnt[k];
+            m_at += mass[k];
         }
-    };
-    int n_all;
-    double total;
-    ask(1u, n_all, total);
-    // Largest key t such that the ids at or above it reach a count (by_count) or a mass (strictly: go beyond it); how many of
-    // the ids at t it takes, and the mass up to them.
-    struct Cut {
-        uint32_t t;
-        int above, take;
-        double mass;
-    };
-    const auto search = [&](bool by_count, bool strict, double target) {
-        uint32_t t = 0;
-        int c;
-        double m;
-        for (int bit = 31; bit >= 0; bit--) {
-            ask(t | (1u << bit), c, m);
-            if (by_count ? c >= target : strict ? m > target : m >= target) t |= 1u << bit;
+        if (tid == 0) {
+            sh.pub_count[turn] = c_all;
+            sh.pub_mass[turn] = m_all;
         }
-        if (t == 0) t = 1;
-        int c0, c1;
-        double m0 = 0, m1;
-        if (t == 0xffffffffu) c0 = 0;
-        else ask(t + 1, c0, m0);
-        ask(t, c1, m1);
-        Cut r;
-        const double w = weight(t);
-        r.t = t;
-        r.above = c0;
-        const double need = by_count ? target - c0 : (target - m0) / w;
-        r.take = (int)fmin(fmax(strict ? floor(need) + 1 : ceil(need), 1.0), (double)(c1 - c0));
-        r.mass = m0 + r.take * w;
-        return r;
-    };
-    uint32_t v = top;
-    int nth = 0;  // the drawn id is this one, in the order of ids, of those at v
-    if (!greedy) {
-        int keep = n_all;
-        double kept = total;
-        const int k = a.top_k ? a.top_k[row] : 0;
-        if (k > 0 && k < keep) {
-            const Cut c = search(true, false, k);
-            keep = k;
-            kept = c.mass;
-        }
-        const float top_p = a.top_p ? a.top_p[row] : 1.f, min_p = a.min_p ? a.min_p[row] : 0.f;
-        if (top_p <= 0.f) {
-            keep = 1;
-            kept = 1;
-        } else if (top_p < 1.f) {
-            const Cut c = search(false, false, (double)top_p * kept);
-            if (c.above + c.take < keep) {
-                keep = c.above + c.take;
-                kept = c.mass;
+        Cl::sync();
+        if (tid == 0) {
+            sh.all_count[0] = 0;
+            sh.all_mass[0] = 0;
+            for (int r = 0; r < C; r++) {
+                sh.all_count[r + 1] = sh.all_count[r] + *Cl::of(&sh.pub_count[turn], r);
+                sh.all_mass[r + 1] = sh.all_mass[r] + *Cl::of(&sh.pub_mass[turn], r);
             }
         }
-        if (min_p > 0.f) {
-            uint32_t t = 0;  // the largest key that is too light
-            for (int bit = 31; bit >= 0; bit--)
-                if ((t | (1u << bit)) < top && weight(t | (1u << bit)) < (double)min_p) t |= 1u << bit;
-            int c;
-            double m;
-            ask(t + 1, c, m);
+        turn ^= 1;
+        __syncthreads();
+    };
+    // The bin in which the target lies (`found`), ids and mass before it, ids in it.  Every CTA finds out for itself.
+    const auto meets = [](int by, double target, int count, unsigned long long mass) {
+        return by == ST_BY_COUNT ? count >= target : by == ST_BY_MASS ? (double)mass >= target : (double)mass > target;
+    };
+    const auto locate = [&](int by, double target) {
+        int r = 0;
+        while (r < C && !meets(by, target, sh.all_count[r + 1], sh.all_mass[r + 1])) r++;
+        const bool none = r == C;  // (no bin's end meets it, for a rounding's sake: it is the last id's bin)
+        if (none)
+            for (r = C - 1; r > 0 && sh.all_count[r + 1] == sh.all_count[r];) r--;
+        const unsigned long long *masses = Cl::of(own_mass, r), m_here = sh.all_mass[r], m_all = sh.all_mass[r + 1];
+        const int *counts = Cl::of(own_count, r), c_here = sh.all_count[r], c_all = sh.all_count[r + 1];
+        for (int b = tid; b < OWN; b += ST_THREADS) {
+            const int c0 = c_here + counts[b], c1 = b + 1 < OWN ? c_here + counts[b + 1] : c_all;
+            const unsigned long long m0 = m_here + masses[b], m1 = b + 1 < OWN ? m_here + masses[b + 1] : m_all;
+            if (none ? c1 > c0 && c1 == c_all : meets(by, target, c1, m1) && !meets(by, target, c0, m0)) {
+                sh.found = r * OWN + b;
+                sh.found_cnt = c0;
+                sh.found_mass = m0;
+                sh.found_n = c1 - c0;
+            }
+        }
+        __syncthreads();
+    };
+    fill([&](uint32_t, double y) { return bin_of(y); });
+    add_up([&](int b) { return b == ST_BINS - 1 ? 0.0 : exp(-(double)b / s); });
+    const double log_total = log((double)sh.all_mass[C] / ST_UNIT);
+    const int n_live = sh.all_count[C];
+
+    // ---- cuts and the draw
+    int keep = n_live, gathered = -1, gathered_n = 0, g_cnt = 0;
+    unsigned long long kept = sh.all_mass[C], g_mass = 0;
+    bool divided = false;  // the bins are those of a bin that has been divided
+    const int want_k = greedy ? 1 : a.top_k ? a.top_k[row] : 0;
+    const float top_p = a.top_p ? a.top_p[row] : 1.f, min_p = a.min_p ? a.min_p[row] : 0.f, u = a.uniforms[row];
+    const auto clear_bins = [&]() {
+        __syncthreads();
+        for (int b = tid; b < 2 * ST_BINS; b += ST_THREADS) bin_lo[b] = 0u;
+        __syncthreads();
+    };
+    for (int step = 0; step < 4; step++) {
+        int by;
+        double target;
+        if (step == 0) {
+            if (want_k <= 0 || want_k >= keep) continue;
+            by = ST_BY_COUNT;
+            target = want_k;
+        } else if (step == 1) {
+            if (greedy || !(top_p < 1.f)) continue;
+            by = ST_BY_MASS;
+            target = (double)top_p * (double)kept;
+            if (!(top_p > 0.f)) {
+                by = ST_BY_COUNT;
+                target = 1;
+            }
+        } else if (step == 2) {
+            if (greedy || !(min_p > 0.f)) continue;
+            if (min_p > 1.f) {
+                keep = 1;
+                continue;
+            }
+            // the smallest logit that is heavy enough, five bits of its key at a time
+            uint32_t light = 0;  // the largest key that is too light (weights rise with the keys)
+            for (int shift = 27;; shift = max(shift - 5, 0)) {
+                const uint32_t step_of = (uint32_t)lane << shift;
+                const uint32_t k = light + step_of;
+                const bool is_light = k >= light && k < top && exp(log_weight(k)) < (double)min_p;
+                light += (uint32_t)(31 - __clz(__ballot_sync(0xffffffffu, is_light) | 1u)) << shift;
+                if (shift == 0) break;
+            }
+            // ids and mass above it, added up in a fixed order
+            int c = 0;
+            unsigned long long m = 0;
+            for (int i = tid; i < mine; i += ST_THREADS) {
+                const uint32_t k = slice[i] == ST_DEAD ? 0u : st_key(slice[i]);
+                if (k > light) {
+                    c++;
+                    m += mass_of(k);
+                }
+            }
+            for (int o = 16; o > 0; o >>= 1) {
+                c += __shfl_xor_sync(0xffffffffu, c, o);
+                m += __shfl_xor_sync(0xffffffffu, m, o);
+            }
+            __syncthreads();
+            if (lane == 0) {
+                sh.wcnt[warp] = c;
+                sh.wsum[warp] = m;
+            }
+            __syncthreads();
+            if (tid == 0) {
+                c = 0;
+                m = 0;
+                for (int w = 0; w < ST_WARPS; w++) {
+                    c += sh.wcnt[w];
+                    m += sh.wsum[w];
+                }
+                sh.pub_count[turn] = c;
+                sh.pub_mass[turn] = m;
+            }
+            Cl::sync();
+            c = 0;
+            m = 0;
+            for (int r = 0; r < C; r++) {
+                c += *Cl::of(&sh.pub_count[turn], r);
+                m += *Cl::of(&sh.pub_mass[turn], r);
+            }
+            turn ^= 1;
             if (c < keep) {
                 keep = c;
                 kept = m;
             }
+            continue;
+        } else {
+            by = ST_BEYOND;
+            target = (u > 0.f ? fmin((double)u, 1.0 - 1.0 / 16777216) : 0.0) * (double)kept;
+            if (keep == 1) {
+                by = ST_BY_COUNT;
+                target = 1;
+            }
         }
-        const float u = a.uniforms[row];
-        const double uu = u > 0.f ? fmin((double)u, 1.0 - 1.0 / 16777216) : 0.0;
-        const Cut c = search(false, true, uu * kept);
-        v = c.t;
-        nth = min(c.take, keep - c.above) - 1;
-        nth = max(nth, 0);
-    }
-    // the nth id at v
-    int before = 0;
-    for (int i0 = lo; i0 < hi; i0 += ST_SIMPLE_THREADS) {
-        const int i = i0 + tid;
-        const bool is = i < hi && st_key(st_load<TYPE>(a.logits, base + i)) == v;
-        const uint32_t b = __ballot_sync(0xffffffffu, is);
+        if (divided) {  // back to the bins of the whole row
+            clear_bins();
+            fill([&](uint32_t, double y) { return bin_of(y); });
+            add_up([&](int b) { return b == ST_BINS - 1 ? 0.0 : exp(-(double)b / s); });
+            divided = false;
+            gathered = -1;
+        }
+        locate(by, target);
+        if (step == 3 && sh.found_cnt >= keep) {  // a rounding beyond the kept ids: the last of them
+            __syncthreads();
+            by = ST_BY_COUNT;
+            target = keep;
+            locate(by, target);
+        }
+        const int bin = sh.found;
+        int before = sh.found_cnt, in = sh.found_n;
+        unsigned long long mass_before = sh.found_mass;
+        uint32_t k_lo = 1u, k_hi = ~0u;  // of the bin's ids, those with these keys
+        const double e_bin = bin == ST_BINS - 1 ? 0.0 : exp(-(double)bin / s);
+        const auto inside = [&](uint32_t bits, double y) {
+            const uint32_t k = st_key(bits);
+            return bin_of(y) == bin && k >= k_lo && k <= k_hi;
+        };
         __syncthreads();
-        if (lane == 0) wi[warp] = __popc(b);
-        __syncthreads();
-        int mine = before + __popc(b & ((1u << lane) - 1u));
-        for (int w = 0; w < 32; w++) {
-            if (w < warp) mine += wi[w];
-            before += wi[w];
+        if (!(bin == gathered && !divided)) {
+            while (in > ST_FEW && k_lo != k_hi) {
+                // too many to rank: divided by the bits of their logits
+                gathered = -1;
+                if (!divided) {
+                    kmax = 0u;
+                    kmin = ~0u;
+                    for (int i = tid; i < mine; i += ST_THREADS)
+                        if (slice[i] != ST_DEAD && inside(slice[i], place(slice[i]))) {
+                            kmax = max(kmax, st_key(slice[i]));
+                            kmin = min(kmin, st_key(slice[i]));
+                        }
+                    __syncthreads();
+                    max_min();
+                    k_lo = kmin;
+                    k_hi = kmax;
+                    if (k_lo == k_hi) break;
+                }
+                divided = true;
+                const int shift = max(0, 32 - __clz(k_hi - k_lo) - 11);  // 2,048 bins cover k_hi - k_lo < 2^(shift + 11)
+                clear_bins();
+                fill([&](uint32_t bits, double y) { return inside(bits, y) ? (int)((k_hi - st_key(bits)) >> shift) : -1; });
+                add_up([&](int) { return e_bin; });
+                const int b_all = before;
+                const unsigned long long m_all = mass_before;
+                locate(by, target - (by == ST_BY_COUNT ? (double)b_all : (double)m_all));
+                before = b_all + sh.found_cnt;
+                mass_before = m_all + sh.found_mass;
+                in = sh.found_n;
+                k_hi = k_hi - ((uint32_t)sh.found << shift);
+                k_lo = max(k_lo, k_hi - ((1u << shift) - 1u));
+                __syncthreads();
+            }
+            if (in <= ST_FEW) {
+                // gathered, ranked by counting, and added up
+                if (tid == 0) sh.list_n[turn] = 0;
+                __syncthreads();
+                for (int i = tid; i < mine; i += ST_THREADS) {
+                    const uint32_t bits = slice[i];
+                    if (bits != ST_DEAD && inside(bits, place(bits))) {
+                        const int at = atomicAdd(&sh.list_n[turn], 1);
+                        if (at < ST_FEW) sh.list[turn][at] = ((unsigned long long)(~st_key(bits)) << 32) | (uint32_t)(beg + i);
+                    }
+                }
+                Cl::sync();
+                int have = 0;
+                unsigned long long me = ~0ull;
+#pragma unroll
+                for (int r = 0; r < C; r++) {
+                    const int m = min(*Cl::of(&sh.list_n[turn], r), ST_FEW);
+                    if (tid >= have && tid < have + m) me = *Cl::of(&sh.list[turn][tid - have], r);
+                    have += m;
+                }
+                turn ^= 1;
+                have = min(have, ST_FEW);
+                static_assert(ST_FEW <= ST_THREADS, "an id a thread");
+                ranked[tid] = me;
+                __syncthreads();
+                int place_of = 0;
+                for (int j = 0; j < have; j++) place_of += ranked[j] < me ? 1 : 0;
+                __syncthreads();
+                if (tid < have) ranked[place_of] = me;
+                __syncthreads();
+                me = tid < have ? ranked[tid] : ~0ull;
+                unsigned long long m = tid < have ? mass_of(~(uint32_t)(me >> 32)) : 0;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const unsigned long long x = __shfl_up_sync(0xffffffffu, m, o);
+                    if (lane >= o) m += x;
+                }
+                if (lane == 31) sh.wsum[warp] = m;
+                __syncthreads();
+                unsigned long long off = 0;
+                for (int w = 0; w < warp; w++) off += sh.wsum[w];
+                ranked_mass[tid] = off + m;
+                gathered = bin;
+                gathered_n = have;
+                g_cnt = before;
+                g_mass = mass_before;
+                __syncthreads();
+            }
         }
-        if (is && mine == nth) {
-            a.token[row] = i;
-            if (a.logprob) a.logprob[row] = (float)((v == top ? 0.0 : ((double)__uint_as_float(st_bits(v)) - z0) * inv_t) - log(total));
+        if (gathered == bin) {
+            before = g_cnt;
+            mass_before = g_mass;
+            // the first of them that meets the target
+            if (tid == 0) {
+                sh.taken = gathered_n;
+                sh.taken_mass = gathered_n ? ranked_mass[gathered_n - 1] : 0;
+            }
+            __syncthreads();
+            if (tid < gathered_n && meets(by, target, before + tid + 1, mass_before + ranked_mass[tid]) &&
+                (tid == 0 || !meets(by, target, before + tid, mass_before + ranked_mass[tid - 1]))) {
+                sh.taken = tid + 1;
+                sh.taken_mass = ranked_mass[tid];
+            }
+            __syncthreads();
+            int taken = sh.taken;
+            if (step < 3) {
+                if (before + taken < keep) {
+                    keep = before + taken;
+                    kept = mass_before + sh.taken_mass;
+                }
+            } else if (rank == 0 && tid == 0) {
+                taken = max(1, min(taken, keep - before));
+                const unsigned long long it = ranked[taken - 1];
+                const uint32_t key = ~(uint32_t)(it >> 32);
+                a.token[row] = lo + (int)(uint32_t)it;
+                if (a.logprob) a.logprob[row] = (float)(log_weight(key) - log_total);
+            }
+            __syncthreads();
+        } else {
+            // all of them are equal: so many of the same weight
+            const unsigned long long w = mass_of(k_lo);
+            const double need = by == ST_BY_COUNT ? target - before : w ? (target - (double)mass_before) / (double)w : (double)in;
+            int taken = (int)fmin(fmax(need, 0.0), (double)in);
+            while (taken > 0 && meets(by, target, before + taken, mass_before + taken * w)) taken--;
+            while (taken < in && !meets(by, target, before + taken, mass_before + taken * w)) taken++;
+            if (step < 3) {
+                if (before + taken < keep) {
+                    keep = before + taken;
+                    kept = mass_before + taken * w;
+                }
+                continue;
+            }
+            taken = max(1, min(taken, keep - before));
+            // the id of the one numbered `taken`: a thread's ids side by side, threads and CTAs in order
+            const int chunk = (mine + ST_THREADS - 1) / ST_THREADS, i0 = min(tid * chunk, mine), i1 = min(i0 + chunk, mine);
+            const uint32_t bits = st_bits(k_lo);
+            int c = 0;
+            for (int i = i0; i < i1; i++) c += slice[i] == bits ? 1 : 0;
+            int in_warp = c;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int x = __shfl_up_sync(0xffffffffu, in_warp, o);
+                if (lane >= o) in_warp += x;
+            }
+            if (lane == 31) sh.wcnt[warp] = in_warp;
+            __syncthreads();
+            int at = in_warp - c, all = 0;
+            for (int x = 0; x < ST_WARPS; x++) {
+                if (x < warp) at += sh.wcnt[x];
+                all += sh.wcnt[x];
+            }
+            if (tid == 0) sh.pub_count[turn] = all;
+            Cl::sync();
+            for (int r = 0; r < rank; r++) at += *Cl::of(&sh.pub_count[turn], r);
+            turn ^= 1;
+            for (int i = i0; i < i1; i++)
+                if (slice[i] == bits && ++at == taken) {
+                    a.token[row] = lo + beg + i;
+                    if (a.logprob) a.logprob[row] = (float)(log_weight(k_lo) - log_total);
+                }
         }
     }
+    Cl::sync();  // nobody leaves while its shared memory may be read
 }
 
+template <int TYPE, int C>
+static cudaError_t launch_settings_form(const sparsk_sample_args &a, cudaStream_t st)
+{
+    static PerDevice<bool> ready_dev;
+    const auto bytes = [](int ids) { return ST_BINS * 8 + ST_BINS / C * 12 + (ids + C - 1) / C * 4; };
+    bool &ready = ready_dev.here();
+    if (!ready) {
+        const cudaError_t e = cudaFuncSetAttribute(settings_sample_kernel<TYPE, C>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes(C * 32768));
+        if (e != cudaSuccess) return e;
+        ready = true;
+    }
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(a.n_rows * C);
+    cfg.blockDim = dim3(ST_THREADS);
+    cfg.dynamicSmemBytes = bytes(a.n_ids);
+    cfg.stream = st;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = C;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = C > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, settings_sample_kernel<TYPE, C>, a);
+}
+template <int TYPE>
+static cudaError_t launch_settings_type(const sparsk_sample_args &a, cudaStream_t st)
+{
+    static_assert(SPARSK_MAX_SAMPLE_IDS <= 8 * 32768, "a CTA counts up to 65,535 ids a bin and holds 32,768");
+    if (a.n_ids <= 8192) return launch_settings_form<TYPE, 1>(a, st);
+    if (a.n_ids <= 32768) return launch_settings_form<TYPE, 4>(a, st);
+    return launch_settings_form<TYPE, 8>(a, st);
+}
 inline cudaError_t launch_settings_sample(const sparsk_sample_args &a, cudaStream_t st)
 {
-    if (a.type == SPARSK_FP32) sample_simple_kernel<SPARSK_FP32><<<a.n_rows, ST_SIMPLE_THREADS, 0, st>>>(a);
-    else if (a.type == SPARSK_BF16) sample_simple_kernel<SPARSK_BF16><<<a.n_rows, ST_SIMPLE_THREADS, 0, st>>>(a);
-    else sample_simple_kernel<SPARSK_FP16><<<a.n_rows, ST_SIMPLE_THREADS, 0, st>>>(a);
-    return cudaGetLastError();
+    if (a.type == SPARSK_FP32) return launch_settings_type<SPARSK_FP32>(a, st);
+    if (a.type == SPARSK_BF16) return launch_settings_type<SPARSK_BF16>(a, st);
+    return launch_settings_type<SPARSK_FP16>(a, st);
 }
 
 }  // namespace sparsk
