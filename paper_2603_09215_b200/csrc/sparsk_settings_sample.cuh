@@ -10,12 +10,12 @@
 // Sums do not depend on the order of the additions: all masses are whole numbers of 2^-44, and within a bin the weights
 // are added as whole numbers too.  With x = s (max - z) / T, bin
 // b = floor(x) and f = x - b, an id weighs e^(-b/s) (1 - h / s), h = s (1 - e^(-f/s)) < 1, and h is added as a number of 32 bits behind
-// the point (s is 51 or more: 2^-38 of the id's weight).  x is worked out in 64 bits, h by five terms of its series
-// (the next one is 2^-38): a draw is decided at the border between two ids, and of a flat row of 150,000 ids each weighs 2^-17, so
+// the point (s is 51 or more: 2^-38 of the id's weight).  x is worked out in 64 bits, h by four terms of its series
+// (the next one is 2^-35 of the id's weight): a draw is decided at the border between two ids, and of a flat row of 150,000 ids each weighs 2^-17, so
 // that 24 bits would draw a neighbour once in a hundred times.  The FP64 units run at half the FP32 rate here.
 //
 // A row is read from memory once, into the shared memory of a cluster of up to eight CTAs.  Counts of a bin and the carries of its
-// h are the halves of one word, so an id costs two shared-memory atomics, which with the eight FP64 operations are what
+// h are the halves of one word, so an id costs two shared-memory atomics, which with the seven FP64 operations are what
 // bounds the kernel where there are many rows; five cluster barriers bound it where there is one.
 #pragma once
 
@@ -53,7 +53,8 @@ __device__ __forceinline__ double st_double(uint32_t bits)
     return __hiloint2double((int)((bits & 0x80000000u) | (((bits & 0x7fffffffu) >> 3) + 0x38000000u)), (int)(bits << 29));
 }
 
-constexpr int ST_THREADS = 512, ST_WARPS = ST_THREADS / 32;
+constexpr int ST_MAX_WARPS = 16;
+constexpr int ST_WIDE_ROWS = 18;  // rows of eight CTAs that find an SM each
 constexpr int ST_BINS = 2048;   // the last one holds what lies beyond the range
 constexpr int ST_FEW = 512;     // ids that are ranked by counting
 constexpr double ST_RANGE = 40;
@@ -73,9 +74,9 @@ struct StShared {
     // this CTA's own
     unsigned long long all_mass[9];      // sums before each CTA of the cluster
     int all_count[9];
-    unsigned long long wsum[ST_WARPS];
-    int wcnt[ST_WARPS];
-    uint32_t wmax[ST_WARPS], wmin[ST_WARPS];
+    unsigned long long wsum[ST_MAX_WARPS];
+    int wcnt[ST_MAX_WARPS];
+    uint32_t wmax[ST_MAX_WARPS], wmin[ST_MAX_WARPS];
     int found, found_cnt, found_n;       // a search's answer: which, ids before it, ids in it
     unsigned long long found_mass;       // mass before it
     int taken;
@@ -98,18 +99,12 @@ struct StCluster {
     }
 };
 
-// Bins' sums: a bin's h in 32 bits and, in the other word, its ids (upper half) and the carries (lower half).
-__device__ __forceinline__ void st_add(uint32_t *lo, uint32_t *hi, int b, uint32_t h)
-{
-    const uint32_t old = atomicAdd(lo + b, h);
-    atomicAdd(hi + b, 0x10000u + (old + h < old ? 1u : 0u));
-}
-
-template <int TYPE, int C>
-static __global__ void __launch_bounds__(ST_THREADS) settings_sample_kernel(sparsk_sample_args a)
+template <int TYPE, int C, int T>
+static __global__ void __launch_bounds__(T, 512 / T) settings_sample_kernel(sparsk_sample_args a)
 {
     typedef StCluster<C> Cl;
-    constexpr int OWN = ST_BINS / C, PER = OWN > ST_THREADS ? OWN / ST_THREADS : 1;  // bins a CTA, a thread adds up
+    constexpr int WARPS = T / 32, OWN = ST_BINS / C, PER = OWN > T ? OWN / T : 1;  // bins a CTA, a thread adds up
+    constexpr int EACH = ST_FEW / T;  // ids to rank, a thread
     extern __shared__ __align__(16) unsigned char st_smem[];
     uint32_t *bin_lo = reinterpret_cast<uint32_t *>(st_smem), *bin_hi = bin_lo + ST_BINS;
     // ranked ids and their masses take the bins' place when these have been added up
@@ -121,20 +116,27 @@ static __global__ void __launch_bounds__(ST_THREADS) settings_sample_kernel(spar
     __shared__ StShared sh;
     const int row = blockIdx.x / C, rank = Cl::rank(), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int lo = a.id_lo ? max(a.id_lo[row], 0) : 0, hi = a.id_hi ? min(a.id_hi[row], a.n_ids) : a.n_ids;
-    const int n = max(hi - lo, 0), per_cta = (n + C - 1) / C, beg = min(rank * per_cta, n), mine = min(per_cta, n - beg);
+    const int n = max(hi - lo, 0), per_cta = (n + C - 1) / C, beg = min(rank * per_cta, n), mine = min(per_cta, n - beg),
+              mine4 = (mine + 3) & ~3;  // (filled up with ids that nobody draws)
+
+    // (asked for before anything waits)
+    const float temp = a.temperature ? a.temperature[row] : 1.f, u = a.uniforms[row];
+    const float top_p = a.top_p ? a.top_p[row] : 1.f, min_p = a.min_p ? a.min_p[row] : 0.f;
+    const int row_k = a.top_k ? a.top_k[row] : 0;
 
     // ---- the row, its largest and smallest logit
-    for (int b = tid; b < 2 * ST_BINS; b += ST_THREADS) bin_lo[b] = 0u;
+    for (int b = tid; b < 2 * ST_BINS; b += T) bin_lo[b] = 0u;
     uint32_t kmax = 0u, kmin = ~0u;
     {
         const long long at = row * a.row_stride + lo + beg;
 #pragma unroll 8
-        for (int i = tid; i < mine; i += ST_THREADS) {
+        for (int i = tid; i < mine; i += T) {
             const uint32_t bits = st_load<TYPE>(a.logits, at + i), k = st_key(bits);
             slice[i] = k ? bits : ST_DEAD;
             kmax = max(kmax, k);
             kmin = min(kmin, k ? k : ~0u);
         }
+        for (int i = mine + tid; i < mine4; i += T) slice[i] = ST_DEAD;
     }
     int turn = 0;  // of what the cluster reads: written anew two turns later, when everybody has passed the barrier between
     const auto max_min = [&]() {
@@ -146,21 +148,16 @@ static __global__ void __launch_bounds__(ST_THREADS) settings_sample_kernel(spar
         }
         __syncthreads();
         if (warp == 0) {
-            kmax = __reduce_max_sync(0xffffffffu, lane < ST_WARPS ? sh.wmax[lane] : 0u);
-            kmin = __reduce_min_sync(0xffffffffu, lane < ST_WARPS ? sh.wmin[lane] : ~0u);
+            kmax = __reduce_max_sync(0xffffffffu, lane < WARPS ? sh.wmax[lane] : 0u);
+            kmin = __reduce_min_sync(0xffffffffu, lane < WARPS ? sh.wmin[lane] : ~0u);
             if (lane == 0) {
                 sh.pub_max[turn] = kmax;
                 sh.pub_min[turn] = kmin;
             }
         }
         Cl::sync();
-        kmax = 0u;
-        kmin = ~0u;
-#pragma unroll
-        for (int r = 0; r < C; r++) {
-            kmax = max(kmax, *Cl::of(&sh.pub_max[turn], r));
-            kmin = min(kmin, *Cl::of(&sh.pub_min[turn], r));
-        }
+        kmax = __reduce_max_sync(0xffffffffu, *Cl::of(&sh.pub_max[turn], lane % C));
+        kmin = __reduce_min_sync(0xffffffffu, *Cl::of(&sh.pub_min[turn], lane % C));
         turn ^= 1;
     };
     max_min();
@@ -173,47 +170,87 @@ static __global__ void __launch_bounds__(ST_THREADS) settings_sample_kernel(spar
         Cl::sync();  // nobody leaves while its shared memory may be read
         return;
     }
-    const float temp = a.temperature ? a.temperature[row] : 1.f;
     const bool greedy = !(temp > 0.f);
     const double z0 = st_double(st_bits(top)), inv_t = greedy ? 1.0 : 1.0 / (double)temp;
     const double range = fmin((z0 - st_double(st_bits(kmin))) * inv_t, ST_RANGE);
     const double s = range > 0 ? (ST_BINS - 1.001) / range : 1.0, scale = s * inv_t;
-    const double c1 = 0.5 / s, c2 = c1 / (3 * s), c3 = c2 / (4 * s), c4 = c3 / (5 * s);
+    const double c1 = 0.5 / s, c2 = c1 / (3 * s), c3 = c2 / (4 * s);
 
     // x of a logit, in ST_POINT's form
     const auto place = [&](uint32_t bits) { return fma(z0 - st_double(bits), scale, ST_POINT); };
     const auto bin_of = [&](double y) { return (int)min((uint32_t)__double2hiint(y) - ST_POINT_HI, (uint32_t)ST_BINS - 1u); };
     const auto h_of = [&](double y) {
         const double f = y - __hiloint2double(__double2hiint(y), 0);
-        return (uint32_t)__double2loint(fma(f, fma(-f, fma(-f, fma(-f, fma(-f, c4, c3), c2), c1), 1.0), ST_POINT));
+        return (uint32_t)__double2loint(fma(f, fma(-f, fma(-f, fma(-f, c3, c2), c1), 1.0), ST_POINT));
     };
     const auto log_weight = [&](uint32_t key) { return key == top ? 0.0 : (st_double(st_bits(key)) - z0) * inv_t; };
     const auto mass_of = [&](uint32_t key) { return __double2ull_rn(exp(log_weight(key)) * ST_UNIT); };
 
     // ---- the bins
-    // Adds the ids for which `which` names a bin into them.  Warps whose ids all fall into one bin add up first.
+    // Adds the ids for which `which` names a bin into them: h in one word, ids (upper half) and carries of h (lower half) in the
+    // other.  Warps whose ids all fall into one bin add up first.
     const auto fill = [&](auto which) {
-#pragma unroll 4
-        for (int i0 = warp * 32; i0 < mine; i0 += ST_THREADS) {
-            const int i = i0 + lane;
-            const uint32_t bits = i < mine ? slice[i] : ST_DEAD;
-            const double y = place(bits);
-            const int b = bits == ST_DEAD ? -1 : which(bits, y);
-            const uint32_t h = bin_of(y) == ST_BINS - 1 ? 0u : h_of(y);
-            const int b0 = __shfl_sync(0xffffffffu, b, 0);
-            if (b0 >= 0 && __all_sync(0xffffffffu, b == b0)) {
-                const uint32_t h_lo = __reduce_add_sync(0xffffffffu, h & 0xffffu), h_hi = __reduce_add_sync(0xffffffffu, h >> 16);
+        for (int i0 = warp * 128; i0 < mine4; i0 += T * 4) {
+            const int i = i0 + lane * 4;
+            const uint4 four = i < mine4 ? *reinterpret_cast<const uint4 *>(slice + i) : make_uint4(ST_DEAD, ST_DEAD, ST_DEAD, ST_DEAD);
+            const uint32_t word[4] = {four.x, four.y, four.z, four.w};
+            int b[4];
+            uint32_t h[4];
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                const double y = place(word[k]);
+                b[k] = word[k] == ST_DEAD ? -1 : which(word[k], y);
+                h[k] = bin_of(y) == ST_BINS - 1 ? 0u : h_of(y);
+            }
+            const int b0 = __shfl_sync(0xffffffffu, b[0], 0);
+            if (b0 >= 0 && __all_sync(0xffffffffu, b[0] == b0 && b[1] == b0 && b[2] == b0 && b[3] == b0)) {
+                uint32_t h_lo = 0, h_hi = 0;
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                    h_lo += h[k] & 0xffffu;
+                    h_hi += h[k] >> 16;
+                }
+                h_lo = __reduce_add_sync(0xffffffffu, h_lo);
+                h_hi = __reduce_add_sync(0xffffffffu, h_hi);
                 if (lane == 0) {
                     const unsigned long long all = ((unsigned long long)h_hi << 16) + h_lo;
-                    const uint32_t part = (uint32_t)all, old = atomicAdd(bin_lo + b, part);
-                    atomicAdd(bin_hi + b, (32u << 16) + (uint32_t)(all >> 32) + (old + part < old ? 1u : 0u));
+                    const uint32_t part = (uint32_t)all, old = atomicAdd(bin_lo + b0, part);
+                    atomicAdd(bin_hi + b0, (128u << 16) + (uint32_t)(all >> 32) + (old + part < old ? 1u : 0u));
                 }
-            } else if (b >= 0) st_add(bin_lo, bin_hi, b, h);
+            } else {
+                uint32_t old[4];
+#pragma unroll
+                for (int k = 0; k < 4; k++)
+                    if (b[k] >= 0) old[k] = atomicAdd(bin_lo + b[k], h[k]);
+#pragma unroll
+                for (int k = 0; k < 4; k++)
+                    if (b[k] >= 0) atomicAdd(bin_hi + b[k], 0x10000u + (old[k] + h[k] < old[k] ? 1u : 0u));
+            }
         }
     };
-    // The cluster's bins added up, this CTA's share of them: ids and mass before each; `e` of a bin is what its ids weigh less h / s.
-    const auto add_up = [&](auto e) {
+    // Calls f(logit, its place here) for the ids of bin `bin`: most others are told by their logit alone, without its x.
+    const auto each_of = [&](int bin, auto f) {
+        double lo_z = -INFINITY, hi_z = INFINITY;
+        if (scale > 0) {
+            if (bin < ST_BINS - 1) lo_z = z0 - (bin + 1.0001) / scale;
+            if (bin > 0) hi_z = z0 - (bin - 0.0001) / scale;
+        }
+        const float zl = __double2float_rd(lo_z), zh = __double2float_ru(hi_z);
+        for (int i = tid * 4; i < mine4; i += T * 4) {
+            const uint4 four = *reinterpret_cast<const uint4 *>(slice + i);
+            const uint32_t word[4] = {four.x, four.y, four.z, four.w};
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                const float z = __uint_as_float(word[k]);  // (what is never drawn is a NaN)
+                if (z >= zl && z <= zh && bin_of(place(word[k])) == bin) f(word[k], i + k);
+            }
+        }
+    };
+    // The cluster's bins added up, this CTA's share of them: ids and mass before each; `e` of a bin is what its ids weigh less h / s, `next` of a
+    // bin by that of the one before.  What lies beyond a whole row's range weighs nothing.
+    const auto add_up = [&](auto e, double next, bool whole_row) {
         Cl::sync();
+        double weigh = tid * PER < OWN ? e(rank * OWN + tid * PER) : 0.0;
         int cnt[PER], c_sum = 0;
         unsigned long long mass[PER], m_sum = 0;
 #pragma unroll
@@ -229,10 +266,11 @@ static __global__ void __launch_bounds__(ST_THREADS) settings_sample_kernel(spar
                     cnt[k] += (int)(w >> 16);
                     h += ((unsigned long long)(w & 0xffffu) << 32) + *Cl::of(bin_lo + b, r);
                 }
-                if (cnt[k]) mass[k] = __double2ull_rn(e(b) * ST_UNIT * ((double)cnt[k] - (double)h * (1.0 / 4294967296.0) / s));
+                if (cnt[k] && (b < ST_BINS - 1 || !whole_row)) mass[k] = __double2ull_rn(weigh * ST_UNIT * ((double)cnt[k] - (double)h * (1.0 / 4294967296.0) / s));
             }
             c_sum += cnt[k];
             m_sum += mass[k];
+            weigh *= next;
         }
         int c_in = c_sum;
         unsigned long long m_in = m_sum;
@@ -253,7 +291,7 @@ static __global__ void __launch_bounds__(ST_THREADS) settings_sample_kernel(spar
         int c_at = 0, c_all = 0;
         unsigned long long m_at = 0, m_all = 0;
 #pragma unroll
-        for (int w = 0; w < ST_WARPS; w++) {
+        for (int w = 0; w < WARPS; w++) {
             if (w == warp) {
                 c_at = c_all;
                 m_at = m_all;
@@ -277,16 +315,65 @@ static __global__ void __launch_bounds__(ST_THREADS) settings_sample_kernel(spar
             sh.pub_mass[turn] = m_all;
         }
         Cl::sync();
-        if (tid == 0) {
-            sh.all_count[0] = 0;
-            sh.all_mass[0] = 0;
-            for (int r = 0; r < C; r++) {
-                sh.all_count[r + 1] = sh.all_count[r] + *Cl::of(&sh.pub_count[turn], r);
-                sh.all_mass[r + 1] = sh.all_mass[r] + *Cl::of(&sh.pub_mass[turn], r);
+        if (warp == 0) {
+            int c = *Cl::of(&sh.pub_count[turn], lane % C);
+            unsigned long long m = *Cl::of(&sh.pub_mass[turn], lane % C);
+#pragma unroll
+            for (int o = 1; o < C; o <<= 1) {
+                const int x = __shfl_up_sync(0xffffffffu, c, o);
+                const unsigned long long y = __shfl_up_sync(0xffffffffu, m, o);
+                if (lane >= o) {
+                    c += x;
+                    m += y;
+                }
+            }
+            if (lane < C) {
+                sh.all_count[lane + 1] = c;
+                sh.all_mass[lane + 1] = m;
+            }
+            if (lane == 0) {
+                sh.all_count[0] = 0;
+                sh.all_mass[0] = 0;
             }
         }
         turn ^= 1;
         __syncthreads();
+    };
+    // One count and one mass of every CTA, added up.
+    const auto sum_up = [&](int &c, unsigned long long &m) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            c += __shfl_xor_sync(0xffffffffu, c, o);
+            m += __shfl_xor_sync(0xffffffffu, m, o);
+        }
+        __syncthreads();
+        if (lane == 0) {
+            sh.wcnt[warp] = c;
+            sh.wsum[warp] = m;
+        }
+        __syncthreads();
+        if (warp == 0) {
+            c = lane < WARPS ? sh.wcnt[lane] : 0;
+            m = lane < WARPS ? sh.wsum[lane] : 0;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                c += __shfl_xor_sync(0xffffffffu, c, o);
+                m += __shfl_xor_sync(0xffffffffu, m, o);
+            }
+            if (lane == 0) {
+                sh.pub_count[turn] = c;
+                sh.pub_mass[turn] = m;
+            }
+        }
+        Cl::sync();
+        c = lane < C ? *Cl::of(&sh.pub_count[turn], lane % C) : 0;
+        m = lane < C ? *Cl::of(&sh.pub_mass[turn], lane % C) : 0;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            c += __shfl_xor_sync(0xffffffffu, c, o);
+            m += __shfl_xor_sync(0xffffffffu, m, o);
+        }
+        turn ^= 1;
     };
     // The bin in which the target lies (`found`), ids and mass before it, ids in it.  Every CTA finds out for itself.
     const auto meets = [](int by, double target, int count, unsigned long long mass) {
@@ -300,7 +387,7 @@ static __global__ void __launch_bounds__(ST_THREADS) settings_sample_kernel(spar
             for (r = C - 1; r > 0 && sh.all_count[r + 1] == sh.all_count[r];) r--;
         const unsigned long long *masses = Cl::of(own_mass, r), m_here = sh.all_mass[r], m_all = sh.all_mass[r + 1];
         const int *counts = Cl::of(own_count, r), c_here = sh.all_count[r], c_all = sh.all_count[r + 1];
-        for (int b = tid; b < OWN; b += ST_THREADS) {
+        for (int b = tid; b < OWN; b += T) {
             const int c0 = c_here + counts[b], c1 = b + 1 < OWN ? c_here + counts[b + 1] : c_all;
             const unsigned long long m0 = m_here + masses[b], m1 = b + 1 < OWN ? m_here + masses[b + 1] : m_all;
             if (none ? c1 > c0 && c1 == c_all : meets(by, target, c1, m1) && !meets(by, target, c0, m0)) {
@@ -313,19 +400,19 @@ static __global__ void __launch_bounds__(ST_THREADS) settings_sample_kernel(spar
         __syncthreads();
     };
     fill([&](uint32_t, double y) { return bin_of(y); });
-    add_up([&](int b) { return b == ST_BINS - 1 ? 0.0 : exp(-(double)b / s); });
-    const double log_total = log((double)sh.all_mass[C] / ST_UNIT);
+    add_up([&](int b) { return exp(-(double)b / s); }, PER > 1 ? exp(-1.0 / s) : 1.0, true);
+    const unsigned long long total = sh.all_mass[C];
+    const auto logprob = [&](uint32_t key) { return (float)(log_weight(key) - log((double)total / ST_UNIT)); };
     const int n_live = sh.all_count[C];
 
     // ---- cuts and the draw
     int keep = n_live, gathered = -1, gathered_n = 0, g_cnt = 0;
-    unsigned long long kept = sh.all_mass[C], g_mass = 0;
+    unsigned long long kept = total, g_mass = 0;
     bool divided = false;  // the bins are those of a bin that has been divided
-    const int want_k = greedy ? 1 : a.top_k ? a.top_k[row] : 0;
-    const float top_p = a.top_p ? a.top_p[row] : 1.f, min_p = a.min_p ? a.min_p[row] : 0.f, u = a.uniforms[row];
+    const int want_k = greedy ? 1 : row_k;
     const auto clear_bins = [&]() {
         __syncthreads();
-        for (int b = tid; b < 2 * ST_BINS; b += ST_THREADS) bin_lo[b] = 0u;
+        for (int b = tid; b < 2 * ST_BINS; b += T) bin_lo[b] = 0u;
         __syncthreads();
     };
     for (int step = 0; step < 4; step++) {
@@ -361,41 +448,14 @@ static __global__ void __launch_bounds__(ST_THREADS) settings_sample_kernel(spar
             // ids and mass above it, added up in a fixed order
             int c = 0;
             unsigned long long m = 0;
-            for (int i = tid; i < mine; i += ST_THREADS) {
+            for (int i = tid; i < mine; i += T) {
                 const uint32_t k = slice[i] == ST_DEAD ? 0u : st_key(slice[i]);
                 if (k > light) {
                     c++;
                     m += mass_of(k);
                 }
             }
-            for (int o = 16; o > 0; o >>= 1) {
-                c += __shfl_xor_sync(0xffffffffu, c, o);
-                m += __shfl_xor_sync(0xffffffffu, m, o);
-            }
-            __syncthreads();
-            if (lane == 0) {
-                sh.wcnt[warp] = c;
-                sh.wsum[warp] = m;
-            }
-            __syncthreads();
-            if (tid == 0) {
-                c = 0;
-                m = 0;
-                for (int w = 0; w < ST_WARPS; w++) {
-                    c += sh.wcnt[w];
-                    m += sh.wsum[w];
-                }
-                sh.pub_count[turn] = c;
-                sh.pub_mass[turn] = m;
-            }
-            Cl::sync();
-            c = 0;
-            m = 0;
-            for (int r = 0; r < C; r++) {
-                c += *Cl::of(&sh.pub_count[turn], r);
-                m += *Cl::of(&sh.pub_mass[turn], r);
-            }
-            turn ^= 1;
+            sum_up(c, m);
             if (c < keep) {
                 keep = c;
                 kept = m;
@@ -412,7 +472,7 @@ static __global__ void __launch_bounds__(ST_THREADS) settings_sample_kernel(spar
         if (divided) {  // back to the bins of the whole row
             clear_bins();
             fill([&](uint32_t, double y) { return bin_of(y); });
-            add_up([&](int b) { return b == ST_BINS - 1 ? 0.0 : exp(-(double)b / s); });
+            add_up([&](int b) { return exp(-(double)b / s); }, PER > 1 ? exp(-1.0 / s) : 1.0, true);
             divided = false;
             gathered = -1;
         }
@@ -427,11 +487,7 @@ static __global__ void __launch_bounds__(ST_THREADS) settings_sample_kernel(spar
         int before = sh.found_cnt, in = sh.found_n;
         unsigned long long mass_before = sh.found_mass;
         uint32_t k_lo = 1u, k_hi = ~0u;  // of the bin's ids, those with these keys
-        const double e_bin = bin == ST_BINS - 1 ? 0.0 : exp(-(double)bin / s);
-        const auto inside = [&](uint32_t bits, double y) {
-            const uint32_t k = st_key(bits);
-            return bin_of(y) == bin && k >= k_lo && k <= k_hi;
-        };
+        const auto inside = [&](uint32_t bits) { return st_key(bits) >= k_lo && st_key(bits) <= k_hi; };
         __syncthreads();
         if (!(bin == gathered && !divided)) {
             while (in > ST_FEW && k_lo != k_hi) {
@@ -440,11 +496,10 @@ static __global__ void __launch_bounds__(ST_THREADS) settings_sample_kernel(spar
                 if (!divided) {
                     kmax = 0u;
                     kmin = ~0u;
-                    for (int i = tid; i < mine; i += ST_THREADS)
-                        if (slice[i] != ST_DEAD && inside(slice[i], place(slice[i]))) {
-                            kmax = max(kmax, st_key(slice[i]));
-                            kmin = min(kmin, st_key(slice[i]));
-                        }
+                    each_of(bin, [&](uint32_t bits, int) {
+                        kmax = max(kmax, st_key(bits));
+                        kmin = min(kmin, st_key(bits));
+                    });
                     __syncthreads();
                     max_min();
                     k_lo = kmin;
@@ -454,8 +509,9 @@ static __global__ void __launch_bounds__(ST_THREADS) settings_sample_kernel(spar
                 divided = true;
                 const int shift = max(0, 32 - __clz(k_hi - k_lo) - 11);  // 2,048 bins cover k_hi - k_lo < 2^(shift + 11)
                 clear_bins();
-                fill([&](uint32_t bits, double y) { return inside(bits, y) ? (int)((k_hi - st_key(bits)) >> shift) : -1; });
-                add_up([&](int) { return e_bin; });
+                const double e_bin = bin == ST_BINS - 1 ? 0.0 : exp(-(double)bin / s);
+                fill([&](uint32_t bits, double y) { return bin_of(y) == bin && inside(bits) ? (int)((k_hi - st_key(bits)) >> shift) : -1; });
+                add_up([&](int) { return e_bin; }, 1.0, false);
                 const int b_all = before;
                 const unsigned long long m_all = mass_before;
                 locate(by, target - (by == ST_BY_COUNT ? (double)b_all : (double)m_all));
@@ -470,44 +526,65 @@ static __global__ void __launch_bounds__(ST_THREADS) settings_sample_kernel(spar
                 // gathered, ranked by counting, and added up
                 if (tid == 0) sh.list_n[turn] = 0;
                 __syncthreads();
-                for (int i = tid; i < mine; i += ST_THREADS) {
-                    const uint32_t bits = slice[i];
-                    if (bits != ST_DEAD && inside(bits, place(bits))) {
-                        const int at = atomicAdd(&sh.list_n[turn], 1);
-                        if (at < ST_FEW) sh.list[turn][at] = ((unsigned long long)(~st_key(bits)) << 32) | (uint32_t)(beg + i);
-                    }
-                }
+                each_of(bin, [&](uint32_t bits, int i) {
+                    if (!inside(bits)) return;
+                    const int at = atomicAdd(&sh.list_n[turn], 1);
+                    if (at < ST_FEW) sh.list[turn][at] = ((unsigned long long)(~st_key(bits)) << 32) | (uint32_t)(beg + i);
+                });
                 Cl::sync();
+                const int from = min(*Cl::of(&sh.list_n[turn], lane % C), ST_FEW);
                 int have = 0;
-                unsigned long long me = ~0ull;
+                unsigned long long me[EACH];
+#pragma unroll
+                for (int q = 0; q < EACH; q++) me[q] = ~0ull;
 #pragma unroll
                 for (int r = 0; r < C; r++) {
-                    const int m = min(*Cl::of(&sh.list_n[turn], r), ST_FEW);
-                    if (tid >= have && tid < have + m) me = *Cl::of(&sh.list[turn][tid - have], r);
+                    const int m = __shfl_sync(0xffffffffu, from, r);
+#pragma unroll
+                    for (int q = 0; q < EACH; q++) {
+                        const int at = tid + q * T - have;
+                        if (at >= 0 && at < m) me[q] = *Cl::of(&sh.list[turn][at], r);
+                    }
                     have += m;
                 }
                 turn ^= 1;
                 have = min(have, ST_FEW);
-                static_assert(ST_FEW <= ST_THREADS, "an id a thread");
-                ranked[tid] = me;
+#pragma unroll
+                for (int q = 0; q < EACH; q++) ranked[tid + q * T] = me[q];
                 __syncthreads();
-                int place_of = 0;
-                for (int j = 0; j < have; j++) place_of += ranked[j] < me ? 1 : 0;
+                int place_of[EACH] = {};
+                if (warp * 32 < have) {
+#pragma unroll 8
+                    for (int j = 0; j < have; j++) {
+                        const unsigned long long other = ranked[j];
+#pragma unroll
+                        for (int q = 0; q < EACH; q++) place_of[q] += other < me[q] ? 1 : 0;
+                    }
+                }
                 __syncthreads();
-                if (tid < have) ranked[place_of] = me;
+#pragma unroll
+                for (int q = 0; q < EACH; q++)
+                    if (tid + q * T < have) ranked[place_of[q]] = me[q];
                 __syncthreads();
-                me = tid < have ? ranked[tid] : ~0ull;
-                unsigned long long m = tid < have ? mass_of(~(uint32_t)(me >> 32)) : 0;
+                unsigned long long m[EACH], all = 0;
+#pragma unroll
+                for (int q = 0; q < EACH; q++) {
+                    const int at = tid * EACH + q;
+                    all += at < have ? mass_of(~(uint32_t)(ranked[at] >> 32)) : 0;
+                    m[q] = all;
+                }
+                unsigned long long in_warp = all;
 #pragma unroll
                 for (int o = 1; o < 32; o <<= 1) {
-                    const unsigned long long x = __shfl_up_sync(0xffffffffu, m, o);
-                    if (lane >= o) m += x;
+                    const unsigned long long x = __shfl_up_sync(0xffffffffu, in_warp, o);
+                    if (lane >= o) in_warp += x;
                 }
-                if (lane == 31) sh.wsum[warp] = m;
+                if (lane == 31) sh.wsum[warp] = in_warp;
                 __syncthreads();
-                unsigned long long off = 0;
+                unsigned long long off = in_warp - all;
                 for (int w = 0; w < warp; w++) off += sh.wsum[w];
-                ranked_mass[tid] = off + m;
+#pragma unroll
+                for (int q = 0; q < EACH; q++) ranked_mass[tid * EACH + q] = off + m[q];
                 gathered = bin;
                 gathered_n = have;
                 g_cnt = before;
@@ -524,11 +601,12 @@ static __global__ void __launch_bounds__(ST_THREADS) settings_sample_kernel(spar
                 sh.taken_mass = gathered_n ? ranked_mass[gathered_n - 1] : 0;
             }
             __syncthreads();
-            if (tid < gathered_n && meets(by, target, before + tid + 1, mass_before + ranked_mass[tid]) &&
-                (tid == 0 || !meets(by, target, before + tid, mass_before + ranked_mass[tid - 1]))) {
-                sh.taken = tid + 1;
-                sh.taken_mass = ranked_mass[tid];
-            }
+            for (int j = tid; j < gathered_n; j += T)
+                if (meets(by, target, before + j + 1, mass_before + ranked_mass[j]) &&
+                    (j == 0 || !meets(by, target, before + j, mass_before + ranked_mass[j - 1]))) {
+                    sh.taken = j + 1;
+                    sh.taken_mass = ranked_mass[j];
+                }
             __syncthreads();
             int taken = sh.taken;
             if (step < 3) {
@@ -541,7 +619,7 @@ static __global__ void __launch_bounds__(ST_THREADS) settings_sample_kernel(spar
                 const unsigned long long it = ranked[taken - 1];
                 const uint32_t key = ~(uint32_t)(it >> 32);
                 a.token[row] = lo + (int)(uint32_t)it;
-                if (a.logprob) a.logprob[row] = (float)(log_weight(key) - log_total);
+                if (a.logprob) a.logprob[row] = logprob(key);
             }
             __syncthreads();
         } else {
@@ -560,7 +638,7 @@ static __global__ void __launch_bounds__(ST_THREADS) settings_sample_kernel(spar
             }
             taken = max(1, min(taken, keep - before));
             // the id of the one numbered `taken`: a thread's ids side by side, threads and CTAs in order
-            const int chunk = (mine + ST_THREADS - 1) / ST_THREADS, i0 = min(tid * chunk, mine), i1 = min(i0 + chunk, mine);
+            const int chunk = (mine + T - 1) / T, i0 = min(tid * chunk, mine), i1 = min(i0 + chunk, mine);
             const uint32_t bits = st_bits(k_lo);
             int c = 0;
             for (int i = i0; i < i1; i++) c += slice[i] == bits ? 1 : 0;
@@ -573,38 +651,38 @@ static __global__ void __launch_bounds__(ST_THREADS) settings_sample_kernel(spar
             if (lane == 31) sh.wcnt[warp] = in_warp;
             __syncthreads();
             int at = in_warp - c, all = 0;
-            for (int x = 0; x < ST_WARPS; x++) {
+            for (int x = 0; x < WARPS; x++) {
                 if (x < warp) at += sh.wcnt[x];
                 all += sh.wcnt[x];
             }
             if (tid == 0) sh.pub_count[turn] = all;
             Cl::sync();
-            for (int r = 0; r < rank; r++) at += *Cl::of(&sh.pub_count[turn], r);
+            at += __reduce_add_sync(0xffffffffu, lane < rank ? *Cl::of(&sh.pub_count[turn], lane % C) : 0);
             turn ^= 1;
             for (int i = i0; i < i1; i++)
                 if (slice[i] == bits && ++at == taken) {
                     a.token[row] = lo + beg + i;
-                    if (a.logprob) a.logprob[row] = (float)(log_weight(k_lo) - log_total);
+                    if (a.logprob) a.logprob[row] = logprob(k_lo);
                 }
         }
     }
     Cl::sync();  // nobody leaves while its shared memory may be read
 }
 
-template <int TYPE, int C>
+template <int TYPE, int C, int T>
 static cudaError_t launch_settings_form(const sparsk_sample_args &a, cudaStream_t st)
 {
     static PerDevice<bool> ready_dev;
-    const auto bytes = [](int ids) { return ST_BINS * 8 + ST_BINS / C * 12 + (ids + C - 1) / C * 4; };
+    const auto bytes = [](int ids) { return ST_BINS * 8 + ST_BINS / C * 12 + ((ids + C - 1) / C + 3) / 4 * 16; };
     bool &ready = ready_dev.here();
     if (!ready) {
-        const cudaError_t e = cudaFuncSetAttribute(settings_sample_kernel<TYPE, C>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes(C * 32768));
+        const cudaError_t e = cudaFuncSetAttribute(settings_sample_kernel<TYPE, C, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes(C * 32768));
         if (e != cudaSuccess) return e;
         ready = true;
     }
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(a.n_rows * C);
-    cfg.blockDim = dim3(ST_THREADS);
+    cfg.blockDim = dim3(T);
     cfg.dynamicSmemBytes = bytes(a.n_ids);
     cfg.stream = st;
     cudaLaunchAttribute attr{};
@@ -613,15 +691,16 @@ static cudaError_t launch_settings_form(const sparsk_sample_args &a, cudaStream_
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = C > 1 ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, settings_sample_kernel<TYPE, C>, a);
+    return cudaLaunchKernelEx(&cfg, settings_sample_kernel<TYPE, C, T>, a);
 }
 template <int TYPE>
 static cudaError_t launch_settings_type(const sparsk_sample_args &a, cudaStream_t st)
 {
     static_assert(SPARSK_MAX_SAMPLE_IDS <= 8 * 32768, "a CTA counts up to 65,535 ids a bin and holds 32,768");
-    if (a.n_ids <= 8192) return launch_settings_form<TYPE, 1>(a, st);
-    if (a.n_ids <= 32768) return launch_settings_form<TYPE, 4>(a, st);
-    return launch_settings_form<TYPE, 8>(a, st);
+    if (a.n_ids <= 8192) return launch_settings_form<TYPE, 1, 512>(a, st);
+    if (a.n_ids <= 32768) return launch_settings_form<TYPE, 4, 512>(a, st);
+    if (a.n_rows <= ST_WIDE_ROWS) return launch_settings_form<TYPE, 8, 512>(a, st);
+    return launch_settings_form<TYPE, 8, 256>(a, st);
 }
 inline cudaError_t launch_settings_sample(const sparsk_sample_args &a, cudaStream_t st)
 {
