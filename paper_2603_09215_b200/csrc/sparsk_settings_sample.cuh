@@ -35,16 +35,17 @@ __device__ __forceinline__ uint32_t st_key(uint32_t bits)
     return (bits & 0x80000000u) ? ~bits : (bits | 0x80000000u);
 }
 __device__ __forceinline__ uint32_t st_bits(uint32_t key) { return (key & 0x80000000u) ? (key & 0x7fffffffu) : ~key; }
+// The bits of a 16-bit number as those of an fp32 number
+template <int TYPE>
+__device__ __forceinline__ uint32_t st_widen(uint32_t h)
+{
+    return TYPE == SPARSK_BF16 ? h << 16 : __float_as_uint(__half2float(__ushort_as_half((unsigned short)h)));
+}
 template <int TYPE>
 __device__ __forceinline__ uint32_t st_load(const void *p, long long at)
 {
-    uint32_t bits;
-    if (TYPE == SPARSK_FP32) bits = reinterpret_cast<const uint32_t *>(p)[at];
-    else {
-        const uint16_t h = reinterpret_cast<const uint16_t *>(p)[at];
-        bits = TYPE == SPARSK_BF16 ? (uint32_t)h << 16 : __float_as_uint(__half2float(__ushort_as_half(h)));
-    }
-    return (bits << 1) == 0u ? 0u : bits;  // the two zeros are one number
+    if (TYPE == SPARSK_FP32) return reinterpret_cast<const uint32_t *>(p)[at];
+    return st_widen<TYPE>(reinterpret_cast<const uint16_t *>(p)[at]);
 }
 // The number as a double, by its bits (the conversion instruction runs at a quarter of the rate): infinity becomes 2^128,
 // zero 2^-127, which is all the same to the weights.
@@ -54,7 +55,6 @@ __device__ __forceinline__ double st_double(uint32_t bits)
 }
 
 constexpr int ST_MAX_WARPS = 16;
-constexpr int ST_WIDE_ROWS = 18;  // rows of eight CTAs that find an SM each
 constexpr int ST_BINS = 2048;   // the last one holds what lies beyond the range
 constexpr int ST_FEW = 512;     // ids that are ranked by counting
 constexpr double ST_RANGE = 40;
@@ -128,13 +128,33 @@ static __global__ void __launch_bounds__(T, 512 / T) settings_sample_kernel(spar
     for (int b = tid; b < 2 * ST_BINS; b += T) bin_lo[b] = 0u;
     uint32_t kmax = 0u, kmin = ~0u;
     {
+        constexpr int ES = TYPE == SPARSK_FP32 ? 4 : 2, WIDE = 16 / ES;
         const long long at = row * a.row_stride + lo + beg;
-#pragma unroll 8
-        for (int i = tid; i < mine; i += T) {
-            const uint32_t bits = st_load<TYPE>(a.logits, at + i), k = st_key(bits);
+        const auto take = [&](int i, uint32_t bits) {
+            bits = (bits << 1) == 0u ? 0u : bits;  // the two zeros are one number
+            const uint32_t k = st_key(bits);
             slice[i] = k ? bits : ST_DEAD;
             kmax = max(kmax, k);
             kmin = min(kmin, k ? k : ~0u);
+        };
+        // single ids up to a 16-byte boundary and behind the last one
+        const unsigned char *src = reinterpret_cast<const unsigned char *>(a.logits) + at * ES;
+        const int ahead = min(mine, (int)((16 - ((uintptr_t)src & 15)) & 15) / ES), wide = (mine - ahead) / WIDE;
+        if (tid < ahead) take(tid, st_load<TYPE>(a.logits, at + tid));
+        for (int i = ahead + wide * WIDE + tid; i < mine; i += T) take(i, st_load<TYPE>(a.logits, at + i));
+        const uint4 *body = reinterpret_cast<const uint4 *>(src + ahead * ES);
+#pragma unroll 4
+        for (int i = tid; i < wide; i += T) {
+            const uint4 x = body[i];
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                if (TYPE == SPARSK_FP32) take(ahead + i * 4 + k, w[k]);
+                else {
+                    take(ahead + i * 8 + k * 2, st_widen<TYPE>(w[k] & 0xffffu));
+                    take(ahead + i * 8 + k * 2 + 1, st_widen<TYPE>(w[k] >> 16));
+                }
+            }
         }
         for (int i = mine + tid; i < mine4; i += T) slice[i] = ST_DEAD;
     }
@@ -190,9 +210,11 @@ static __global__ void __launch_bounds__(T, 512 / T) settings_sample_kernel(spar
     // Adds the ids for which `which` names a bin into them: h in one word, ids (upper half) and carries of h (lower half) in the
     // other.  Warps whose ids all fall into one bin add up first.
     const auto fill = [&](auto which) {
+        const auto at = [&](int i) { return i < mine4 ? *reinterpret_cast<const uint4 *>(slice + i) : make_uint4(ST_DEAD, ST_DEAD, ST_DEAD, ST_DEAD); };
+        uint4 after = at(tid * 4);
         for (int i0 = warp * 128; i0 < mine4; i0 += T * 4) {
-            const int i = i0 + lane * 4;
-            const uint4 four = i < mine4 ? *reinterpret_cast<const uint4 *>(slice + i) : make_uint4(ST_DEAD, ST_DEAD, ST_DEAD, ST_DEAD);
+            const uint4 four = after;
+            after = at(i0 + lane * 4 + T * 4);  // (ahead of this round's atomics)
             const uint32_t word[4] = {four.x, four.y, four.z, four.w};
             int b[4];
             uint32_t h[4];
@@ -228,21 +250,49 @@ static __global__ void __launch_bounds__(T, 512 / T) settings_sample_kernel(spar
             }
         }
     };
-    // Calls f(logit, its place here) for the ids of bin `bin`: most others are told by their logit alone, without its x.
-    const auto each_of = [&](int bin, auto f) {
-        double lo_z = -INFINITY, hi_z = INFINITY;
-        if (scale > 0) {
-            if (bin < ST_BINS - 1) lo_z = z0 - (bin + 1.0001) / scale;
-            if (bin > 0) hi_z = z0 - (bin - 0.0001) / scale;
+    // The largest key below the top for which `holds`, which no larger one may follow; 0 if none does.  Five bits at a time.
+    const auto last_key = [&](auto holds) {
+        uint32_t at = 0;
+        for (int shift = 27;; shift = max(shift - 5, 0)) {
+            const uint32_t k = at + ((uint32_t)lane << shift);
+            const bool yes = k > at && k < top && holds(k);
+            at += (uint32_t)(31 - __clz(__ballot_sync(0xffffffffu, yes) | 1u)) << shift;
+            if (shift == 0) return at;
         }
-        const float zl = __double2float_rd(lo_z), zh = __double2float_ru(hi_z);
-        for (int i = tid * 4; i < mine4; i += T * 4) {
-            const uint4 four = *reinterpret_cast<const uint4 *>(slice + i);
-            const uint32_t word[4] = {four.x, four.y, four.z, four.w};
+    };
+    // The keys of bin `bin`'s logits, the smallest and the largest.  The places rise and fall with the keys, so that they are
+    // a stretch; its ends are a rounding or two from where the bin's borders lie, and 32 lanes look at 32 keys there.
+    const auto keys_of = [&](int bin, uint32_t &k_lo, uint32_t &k_hi) {
+        const auto edge = [&](double x) {  // the smallest key whose place is below x, for a whole number x
+            const float z = (float)(z0 - x / scale);
+            const auto below = [&](uint32_t k) { return place(st_bits(k)) < ST_POINT + x; };
+            const uint32_t k = max(st_key(__float_as_uint(z)), 17u) - 16u;
+            const uint32_t b = __ballot_sync(0xffffffffu, below(min(k + lane, top)));
+            if (b && !(b & 1u)) return min(k + __ffs(b) - 1, top);
+            return last_key([&](uint32_t i) { return !below(i); }) + 1u;  // (numbers around zero are much finer than the places)
+        };
+        k_lo = bin == ST_BINS - 1 || !(scale > 0) ? 1u : edge(bin + 1);
+        k_hi = bin == 0 || !(scale > 0) ? top : edge(bin) - 1u;
+    };
+    // Calls f(key, place in the slice) for the ids with keys from k_lo to k_hi.
+    const auto each_of = [&](uint32_t k_lo, uint32_t k_hi, auto f) {
+        const auto key_of = [](uint32_t word) { return word ^ ((uint32_t)((int)word >> 31) | 0x80000000u); };  // (0 for what is never drawn)
+        for (int i = tid * 4; i < mine4; i += T * 16) {
+            // sixteen ids at a time, so that their loads do not wait for what f writes
+            uint4 four[4];
 #pragma unroll
-            for (int k = 0; k < 4; k++) {
-                const float z = __uint_as_float(word[k]);  // (what is never drawn is a NaN)
-                if (z >= zl && z <= zh && bin_of(place(word[k])) == bin) f(word[k], i + k);
+            for (int q = 0; q < 4; q++)
+                four[q] = i + q * T * 4 < mine4 ? *reinterpret_cast<const uint4 *>(slice + i + q * T * 4) : make_uint4(ST_DEAD, ST_DEAD, ST_DEAD, ST_DEAD);
+            uint32_t hits = 0;
+#pragma unroll
+            for (int q = 0; q < 4; q++) {
+                const uint32_t word[4] = {four[q].x, four[q].y, four[q].z, four[q].w};
+#pragma unroll
+                for (int k = 0; k < 4; k++) hits |= key_of(word[k]) - k_lo <= k_hi - k_lo ? 1u << (q * 4 + k) : 0u;
+            }
+            for (; hits; hits &= hits - 1) {
+                const int k = __ffs(hits) - 1, at = i + (k >> 2) * T * 4 + (k & 3);
+                f(key_of(slice[at]), at);
             }
         }
     };
@@ -436,25 +486,15 @@ static __global__ void __launch_bounds__(T, 512 / T) settings_sample_kernel(spar
                 keep = 1;
                 continue;
             }
-            // the smallest logit that is heavy enough, five bits of its key at a time
-            uint32_t light = 0;  // the largest key that is too light (weights rise with the keys)
-            for (int shift = 27;; shift = max(shift - 5, 0)) {
-                const uint32_t step_of = (uint32_t)lane << shift;
-                const uint32_t k = light + step_of;
-                const bool is_light = k >= light && k < top && exp(log_weight(k)) < (double)min_p;
-                light += (uint32_t)(31 - __clz(__ballot_sync(0xffffffffu, is_light) | 1u)) << shift;
-                if (shift == 0) break;
-            }
+            // the largest logit that is too light
+            const uint32_t light = last_key([&](uint32_t k) { return exp(log_weight(k)) < (double)min_p; });
             // ids and mass above it, added up in a fixed order
             int c = 0;
             unsigned long long m = 0;
-            for (int i = tid; i < mine; i += T) {
-                const uint32_t k = slice[i] == ST_DEAD ? 0u : st_key(slice[i]);
-                if (k > light) {
-                    c++;
-                    m += mass_of(k);
-                }
-            }
+            each_of(light + 1u, top, [&](uint32_t k, int) {
+                c++;
+                m += mass_of(k);
+            });
             sum_up(c, m);
             if (c < keep) {
                 keep = c;
@@ -486,8 +526,8 @@ static __global__ void __launch_bounds__(T, 512 / T) settings_sample_kernel(spar
         const int bin = sh.found;
         int before = sh.found_cnt, in = sh.found_n;
         unsigned long long mass_before = sh.found_mass;
-        uint32_t k_lo = 1u, k_hi = ~0u;  // of the bin's ids, those with these keys
-        const auto inside = [&](uint32_t bits) { return st_key(bits) >= k_lo && st_key(bits) <= k_hi; };
+        uint32_t k_lo, k_hi;  // the ids in question are those with keys from here to there
+        keys_of(bin, k_lo, k_hi);
         __syncthreads();
         if (!(bin == gathered && !divided)) {
             while (in > ST_FEW && k_lo != k_hi) {
@@ -496,9 +536,9 @@ static __global__ void __launch_bounds__(T, 512 / T) settings_sample_kernel(spar
                 if (!divided) {
                     kmax = 0u;
                     kmin = ~0u;
-                    each_of(bin, [&](uint32_t bits, int) {
-                        kmax = max(kmax, st_key(bits));
-                        kmin = min(kmin, st_key(bits));
+                    each_of(k_lo, k_hi, [&](uint32_t k, int) {
+                        kmax = max(kmax, k);
+                        kmin = min(kmin, k);
                     });
                     __syncthreads();
                     max_min();
@@ -510,7 +550,7 @@ static __global__ void __launch_bounds__(T, 512 / T) settings_sample_kernel(spar
                 const int shift = max(0, 32 - __clz(k_hi - k_lo) - 11);  // 2,048 bins cover k_hi - k_lo < 2^(shift + 11)
                 clear_bins();
                 const double e_bin = bin == ST_BINS - 1 ? 0.0 : exp(-(double)bin / s);
-                fill([&](uint32_t bits, double y) { return bin_of(y) == bin && inside(bits) ? (int)((k_hi - st_key(bits)) >> shift) : -1; });
+                fill([&](uint32_t bits, double) { return st_key(bits) - k_lo <= k_hi - k_lo ? (int)((k_hi - st_key(bits)) >> shift) : -1; });
                 add_up([&](int) { return e_bin; }, 1.0, false);
                 const int b_all = before;
                 const unsigned long long m_all = mass_before;
@@ -526,10 +566,9 @@ static __global__ void __launch_bounds__(T, 512 / T) settings_sample_kernel(spar
                 // gathered, ranked by counting, and added up
                 if (tid == 0) sh.list_n[turn] = 0;
                 __syncthreads();
-                each_of(bin, [&](uint32_t bits, int i) {
-                    if (!inside(bits)) return;
+                each_of(k_lo, k_hi, [&](uint32_t k, int i) {
                     const int at = atomicAdd(&sh.list_n[turn], 1);
-                    if (at < ST_FEW) sh.list[turn][at] = ((unsigned long long)(~st_key(bits)) << 32) | (uint32_t)(beg + i);
+                    if (at < ST_FEW) sh.list[turn][at] = ((unsigned long long)(~k) << 32) | (uint32_t)(beg + i);
                 });
                 Cl::sync();
                 const int from = min(*Cl::of(&sh.list_n[turn], lane % C), ST_FEW);
@@ -553,13 +592,16 @@ static __global__ void __launch_bounds__(T, 512 / T) settings_sample_kernel(spar
                 for (int q = 0; q < EACH; q++) ranked[tid + q * T] = me[q];
                 __syncthreads();
                 int place_of[EACH] = {};
-                if (warp * 32 < have) {
-#pragma unroll 8
+                if (have > T) {
+#pragma unroll 4
                     for (int j = 0; j < have; j++) {
                         const unsigned long long other = ranked[j];
 #pragma unroll
                         for (int q = 0; q < EACH; q++) place_of[q] += other < me[q] ? 1 : 0;
                     }
+                } else if (warp * 32 < have) {
+#pragma unroll 8
+                    for (int j = 0; j < have; j++) place_of[0] += ranked[j] < me[0] ? 1 : 0;
                 }
                 __syncthreads();
 #pragma unroll
@@ -699,7 +741,6 @@ static cudaError_t launch_settings_type(const sparsk_sample_args &a, cudaStream_
     static_assert(SPARSK_MAX_SAMPLE_IDS <= 8 * 32768, "a CTA counts up to 65,535 ids a bin and holds 32,768");
     if (a.n_ids <= 8192) return launch_settings_form<TYPE, 1, 512>(a, st);
     if (a.n_ids <= 32768) return launch_settings_form<TYPE, 4, 512>(a, st);
-    if (a.n_rows <= ST_WIDE_ROWS) return launch_settings_form<TYPE, 8, 512>(a, st);
     return launch_settings_form<TYPE, 8, 256>(a, st);
 }
 inline cudaError_t launch_settings_sample(const sparsk_sample_args &a, cudaStream_t st)
