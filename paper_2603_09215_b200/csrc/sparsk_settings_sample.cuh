@@ -437,6 +437,11 @@ static __global__ void __launch_bounds__(T, 512 / T) settings_sample_kernel(spar
             for (r = C - 1; r > 0 && sh.all_count[r + 1] == sh.all_count[r];) r--;
         const unsigned long long *masses = Cl::of(own_mass, r), m_here = sh.all_mass[r], m_all = sh.all_mass[r + 1];
         const int *counts = Cl::of(own_count, r), c_here = sh.all_count[r], c_all = sh.all_count[r + 1];
+        if (tid == 0) {  // (found below in every case; whatever is not would stay inside the arrays)
+            sh.found = sh.found_cnt = sh.found_n = 0;
+            sh.found_mass = 0;
+        }
+        __syncthreads();
         for (int b = tid; b < OWN; b += T) {
             const int c0 = c_here + counts[b], c1 = b + 1 < OWN ? c_here + counts[b + 1] : c_all;
             const unsigned long long m0 = m_here + masses[b], m1 = b + 1 < OWN ? m_here + masses[b + 1] : m_all;
@@ -657,7 +662,7 @@ static __global__ void __launch_bounds__(T, 512 / T) settings_sample_kernel(spar
                     kept = mass_before + sh.taken_mass;
                 }
             } else if (rank == 0 && tid == 0) {
-                taken = max(1, min(taken, keep - before));
+                taken = max(1, min(min(taken, keep - before), gathered_n));
                 const unsigned long long it = ranked[taken - 1];
                 const uint32_t key = ~(uint32_t)(it >> 32);
                 a.token[row] = lo + (int)(uint32_t)it;
