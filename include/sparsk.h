@@ -328,7 +328,7 @@ int sparsk_attention_static(const sparsk_attn_args *args /*host*/, void *cuda_st
 #define SPARSK_PAGES_TABLE 2  /* a sequence needs more than max_blocks pages                      */
 #define SPARSK_PAGES_ROWS 4   /* more new rows than max_rows                                      */
 #define SPARSK_PAGES_BAD 8    /* a negative length, rows below -1, a queue that its ring cannot hold */
-#define SPARSK_MAX_MAP_SEQS 16384
+#define SPARSK_MAX_MAP_SEQS 12288
 typedef struct {
     const int32_t *seq_len, *seq_rows; /* [n_seqs]                                              */
     int32_t *block_table;              /* [n_seqs][max_blocks], rows table_stride numbers apart */

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import NamedTuple
 
 import numpy as np
@@ -93,6 +94,15 @@ class SampleArgs(C.Structure):
                                           "token", "logprob")] + [
         ("row_stride", C.c_int64)] + [(n, C.c_int32) for n in ("type", "n_rows", "n_ids")]
 
+
+# The same blocks packed in one go: filling a ctypes structure field by field costs up to 2 us a call.
+_POOL = "4Q3q5i4x"
+_PACK_MAP = struct.Struct("12Qq5i4x")
+_PACK_APPEND = struct.Struct(_POOL + "7Q8q5i4x")
+_PACK_ATTN = struct.Struct(_POOL + "6Q5q7if")
+_PACK_SAMPLE = struct.Struct("10Qq3i4x")
+for _p, _c in ((_PACK_MAP, PageMapArgs), (_PACK_APPEND, PagedAppendArgs), (_PACK_ATTN, PagedAttnArgs), (_PACK_SAMPLE, SampleArgs)):
+    assert _p.size == C.sizeof(_c), (_p.format, _c)
 
 _lib = None
 
@@ -280,6 +290,13 @@ def _need(ok: bool, what: str):
         raise SparskError(EINVAL, what)
 
 
+def _pack(block: struct.Struct, *fields) -> bytes:
+    try:
+        return block.pack(*fields)
+    except struct.error as e:
+        raise SparskError(EINVAL, f"a size or stride that does not fit its field: {e}") from None
+
+
 def _vec(t: torch.Tensor, dtype, n: int, dev: int, what: str) -> int:
     """Address of a contiguous array of at least n numbers on device `dev`."""
     if t.dtype is not dtype or t.get_device() != dev or t.numel() < n or not t.is_contiguous():
@@ -289,25 +306,26 @@ def _vec(t: torch.Tensor, dtype, n: int, dev: int, what: str) -> int:
 
 def _launch(name: str, dev: int, *args):
     """One entry point, on the current stream of device `dev` whichever device is current."""
+    f = getattr(_lib or load(), name)
     if torch._C._cuda_getDevice() == dev:
-        rc = getattr(load(), name)(*args, torch._C._cuda_getCurrentRawStream(dev))
+        rc = f(*args, torch._C._cuda_getCurrentRawStream(dev))
     else:
         with torch.cuda.device(dev):
-            rc = getattr(load(), name)(*args, torch._C._cuda_getCurrentRawStream(dev))
+            rc = f(*args, torch._C._cuda_getCurrentRawStream(dev))
     if rc != OK:
         raise SparskError(rc, name)
 
 
-def _page_pool(k: torch.Tensor, v: torch.Tensor, k_scale, v_scale) -> PagePool:
-    """Pools as [n_pages, n_kv_heads, page_size, head_dim]; pools whose positions lie before their heads come
+def _page_pool(k: torch.Tensor, v: torch.Tensor, k_scale, v_scale):
+    """(fields of PagePool, device, kv heads, head_dim).  Pools as [n_pages, n_kv_heads, page_size, head_dim]; pools whose positions lie before their heads come
     transposed (`x.transpose(1, 2)`)."""
     dev, shape, st = k.get_device(), k.shape, k.stride()
     _need(dev >= 0 and v.get_device() == dev, "the pools are on one CUDA device")
     _need(len(shape) == 4 and v.shape == shape and v.stride() == st and v.dtype is k.dtype, "pools of one shape, layout and type")
     _need(st[3] == 1, "a head's numbers are contiguous")
-    ks = None if k_scale is None else _vec(k_scale, torch.float32, shape[1], dev, "k_scale")
-    vs = None if v_scale is None else _vec(v_scale, torch.float32, shape[1], dev, "v_scale")
-    return PagePool(k.data_ptr(), v.data_ptr(), ks, vs, st[0], st[1], st[2], _TYPES.get(k.dtype, -1), *shape)
+    ks = 0 if k_scale is None else _vec(k_scale, torch.float32, shape[1], dev, "k_scale")
+    vs = 0 if v_scale is None else _vec(v_scale, torch.float32, shape[1], dev, "v_scale")
+    return ((k.data_ptr(), v.data_ptr(), ks, vs, st[0], st[1], st[2], _TYPES.get(k.dtype, -1), *shape), dev, shape[1], shape[3])
 
 
 def _rows(t: torch.Tensor, n: int, heads: int, head_dim: int, dev: int, what: str):
@@ -343,13 +361,13 @@ def page_map(lens: torch.Tensor, rows: torch.Tensor, block_table: torch.Tensor, 
                   status if status is not None else new(1))
     table, stride, blocks = _table(block_table, n, dev)
     i32 = torch.int32
-    a = PageMapArgs(_vec(lens, i32, n, dev, "lens"), _vec(rows, i32, n, dev, "rows"), table, _vec(ring, i32, 1, dev, "ring"),
-                    _vec(old_queue, i32, 2, dev, "old_queue"), _vec(out.seq_len, i32, n, dev, "seq_len"),
-                    _vec(out.queue, i32, 2, dev, "queue"), _vec(out.row_start, i32, n + 1, dev, "row_start"),
-                    _vec(out.row_seq, i32, m, dev, "row_seq"), _vec(out.row_pos, i32, m, dev, "row_pos"),
-                    _vec(out.slot_map, torch.int64, m, dev, "slot_map"), _vec(out.status, i32, 1, dev, "status"),
-                    stride, n, blocks, page_size, ring.shape[0], m)
-    _launch("sparsk_page_map", dev, C.addressof(a))
+    a = _pack(_PACK_MAP, _vec(lens, i32, n, dev, "lens"), _vec(rows, i32, n, dev, "rows"), table, _vec(ring, i32, 1, dev, "ring"),
+                       _vec(old_queue, i32, 2, dev, "old_queue"), _vec(out.seq_len, i32, n, dev, "seq_len"),
+                       _vec(out.queue, i32, 2, dev, "queue"), _vec(out.row_start, i32, n + 1, dev, "row_start"),
+                       _vec(out.row_seq, i32, m, dev, "row_seq"), _vec(out.row_pos, i32, m, dev, "row_pos"),
+                       _vec(out.slot_map, torch.int64, m, dev, "slot_map"), _vec(out.status, i32, 1, dev, "status"),
+                       stride, n, blocks, page_size, ring.shape[0], m)
+    _launch("sparsk_page_map", dev, a)
     return out
 
 
@@ -359,13 +377,12 @@ def paged_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cach
     """sparsk_paged_append: k, v [n, n_kv_heads, head_dim] into their slots (int64 [n], -1: left out); with
     `rope` [positions, head_dim / 2, 2] (cosine, sine; float32) keys and queries q [n, n_q_heads, head_dim] are turned to
     their positions row_pos (int32 [n]).  Returns the turned queries (q_out, or new: q's type, bf16 for fp32)."""
-    pool = _page_pool(k_cache, v_cache, k_scale, v_scale)
-    dev, n, hk, hd = k_cache.get_device(), k.shape[0], pool.n_kv_heads, pool.head_dim
+    pool, dev, hk, hd = _page_pool(k_cache, v_cache, k_scale, v_scale)
+    n = k.shape[0]
     kp, krs, khs = _rows(k, n, hk, hd, dev, "k")
     vp, vrs, vhs = _rows(v, n, hk, hd, dev, "v")
     _need(v.dtype is k.dtype, "k and v are of one type")
-    qp = qo = rp = rt = None
-    qrs = qhs = qors = qohs = hq = length = 0
+    qp = qo = rp = rt = qrs = qhs = qors = qohs = hq = length = 0
     qot = BF16
     if q is not None:
         hq = q.shape[1]
@@ -380,10 +397,10 @@ def paged_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cach
               "rope: [positions, head_dim / 2, 2], and row_pos with it")
         length = rope.shape[0]
         rt, rp = _vec(rope, torch.float32, 1, dev, "rope"), _vec(row_pos, torch.int32, n, dev, "row_pos")
-    a = PagedAppendArgs(pool, kp, vp, qp, qo, _vec(slot_map, torch.int64, n, dev, "slot_map"), rp, rt, krs, khs, vrs, vhs, qrs, qhs,
-                        qors, qohs, _TYPES.get(k.dtype, -1), qot, n, hq, length)
+    a = _pack(_PACK_APPEND, *pool, kp, vp, qp, qo, _vec(slot_map, torch.int64, n, dev, "slot_map"), rp, rt, krs, khs, vrs, vhs, qrs, qhs,
+                          qors, qohs, _TYPES.get(k.dtype, -1), qot, n, hq, length)
     if n:
-        _launch("sparsk_paged_append", dev, C.addressof(a))
+        _launch("sparsk_paged_append", dev, a)
     return q_out
 
 
@@ -395,25 +412,25 @@ def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     included) positions lie in the pages of block_table (int32 [sequences, blocks]).  Sequence i has rows row_start[i]
     to row_start[i + 1] - 1; without row_start every sequence has one.  max_rows and max_len, where known, size the launch.  `lse`
     (float32 [n, n_q_heads]) receives the logarithms of the softmax sums."""
-    pool = _page_pool(k_cache, v_cache, k_scale, v_scale)
-    dev, n_seqs, (n, hq, hd) = k_cache.get_device(), seq_len.shape[0], q.shape
+    pool, dev, _, head_dim = _page_pool(k_cache, v_cache, k_scale, v_scale)
+    n_seqs, (n, hq, hd) = seq_len.shape[0], q.shape
     if out is None:
         out = torch.empty((n, hq, hd), dtype=q.dtype, device=q.device)
-    _need(out.dtype is q.dtype and hd == pool.head_dim, "q and out are of one type, with the pool's head_dim")
+    _need(out.dtype is q.dtype and hd == head_dim, "q and out are of one type, with the pool's head_dim")
     qp, qrs, qhs = _rows(q, n, hq, hd, dev, "q")
     op, ors, ohs = _rows(out, n, hq, hd, dev, "out")
     table, stride, blocks = _table(block_table, n_seqs, dev)
-    a = PagedAttnArgs(pool, qp, op, None if lse is None else _vec(lse, torch.float32, n * hq, dev, "lse"), table,
-                      _vec(seq_len, torch.int32, n_seqs, dev, "seq_len"),
-                      None if row_start is None else _vec(row_start, torch.int32, n_seqs + 1, dev, "row_start"),
-                      stride, qrs, qhs, ors, ohs, _TYPES.get(q.dtype, -1), n, n_seqs, blocks, hq, max_rows, max_len, scale)
+    a = _pack(_PACK_ATTN, *pool, qp, op, 0 if lse is None else _vec(lse, torch.float32, n * hq, dev, "lse"), table,
+                        _vec(seq_len, torch.int32, n_seqs, dev, "seq_len"),
+                        0 if row_start is None else _vec(row_start, torch.int32, n_seqs + 1, dev, "row_start"),
+                        stride, qrs, qhs, ors, ohs, _TYPES.get(q.dtype, -1), n, n_seqs, blocks, hq, max_rows, max_len, scale)
     if n == 0:
         return out
     if scratch is None:
-        nbytes = load().sparsk_paged_attention_scratch_bytes(C.addressof(a))
+        nbytes = load().sparsk_paged_attention_scratch_bytes(a)
         _need(nbytes > 0, "sparsk_paged_attention: a size, type, stride or address that it does not take")
         scratch = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
-    _launch("sparsk_paged_attention", dev, C.addressof(a), _vec(scratch, torch.uint8, 1, dev, "scratch"), scratch.numel())
+    _launch("sparsk_paged_attention", dev, a, _vec(scratch, torch.uint8, 1, dev, "scratch"), scratch.numel())
     return out
 
 
@@ -426,13 +443,13 @@ def sample(logits: torch.Tensor, uniforms: torch.Tensor, *, temperature=None, to
     _need(dev >= 0 and (ids == 1 or logits.stride(1) == 1), "logits: [rows, ids] on a CUDA device, a row contiguous")
     if token is None:
         token = torch.empty(n, dtype=torch.int32, device=logits.device)
-    f = lambda t, what: None if t is None else _vec(t, torch.float32, n, dev, what)  # noqa: E731
-    i = lambda t, what: None if t is None else _vec(t, torch.int32, n, dev, what)  # noqa: E731
-    a = SampleArgs(logits.data_ptr(), f(uniforms, "uniforms"), f(temperature, "temperature"), f(top_p, "top_p"), f(min_p, "min_p"),
-                   i(top_k, "top_k"), i(id_lo, "id_lo"), i(id_hi, "id_hi"), i(token, "token"), f(logprob, "logprob"),
-                   logits.stride(0), _TYPES.get(logits.dtype, -1), n, ids)
+    f = lambda t, what: 0 if t is None else _vec(t, torch.float32, n, dev, what)  # noqa: E731
+    i = lambda t, what: 0 if t is None else _vec(t, torch.int32, n, dev, what)  # noqa: E731
+    a = _pack(_PACK_SAMPLE, logits.data_ptr(), f(uniforms, "uniforms"), f(temperature, "temperature"), f(top_p, "top_p"), f(min_p, "min_p"),
+                          i(top_k, "top_k"), i(id_lo, "id_lo"), i(id_hi, "id_hi"), i(token, "token"), f(logprob, "logprob"),
+                          logits.stride(0), _TYPES.get(logits.dtype, -1), n, ids)
     if n:
-        _launch("sparsk_sample", dev, C.addressof(a))
+        _launch("sparsk_sample", dev, a)
     return token
 
 

@@ -31,17 +31,19 @@ extern "C" int sparsk_page_map(const sparsk_page_map_args *a, void *cuda_stream)
         const size_t m = out == a->queue_out ? 8 : n;
         if (overlap(out, m, a->seq_len, n) || overlap(out, m, a->seq_rows, n) || overlap(out, m, a->queue, 8)) return SPARSK_EINVAL;
     }
-    const int smem = 3 * (a->n_seqs + 1) * (int)sizeof(int);
+    const int smem = 4 * a->n_seqs * (int)sizeof(int);
     static PerDevice<bool> ready;
     if (!ready.here()) {
         if (cudaFuncSetAttribute(page_map_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 3 * (SPARSK_MAX_MAP_SEQS + 1) * (int)sizeof(int)) != cudaSuccess)
+                                 4 * SPARSK_MAX_MAP_SEQS * (int)sizeof(int)) != cudaSuccess)
             return SPARSK_ECUDA;
         ready.here() = true;
     }
-    // a block for every four rows a thread: the sums that each repeats cost about as much
-    const int grid = std::max(1, std::min(128, (a->max_rows + 4 * PM_THREADS - 1) / (4 * PM_THREADS)));
-    page_map_kernel<<<grid, PM_THREADS, smem, (cudaStream_t)cuda_stream>>>(*a);
+    PageMapArgs p{*a, -1};
+    for (int i = 0; i < 31; i++)
+        if (a->page_size == 1 << i) p.shift = i;
+    const int grid = std::max(1, std::min(256, (a->max_rows + PM_THREADS - 1) / PM_THREADS));  // a row a thread
+    page_map_kernel<<<grid, PM_THREADS, smem, (cudaStream_t)cuda_stream>>>(p);
     return cudaGetLastError() == cudaSuccess ? SPARSK_OK : SPARSK_ECUDA;
 }
 

@@ -33,7 +33,7 @@ def test_page_map_refuses(bad):
 
 def test_page_map_refuses_more_sequences_than_it_holds():
     far = dict(seq_rows=A << 1, queue=A << 2, seq_len_out=A << 3, queue_out=A << 4)
-    assert call("sparsk_page_map", map_args(n_seqs=16385, **far)) == B.ECAPACITY
+    assert call("sparsk_page_map", map_args(n_seqs=12289, **far)) == B.ECAPACITY
     assert B.load().sparsk_page_map(None, None) == B.EINVAL
 
 
