@@ -166,7 +166,7 @@ extern "C" int sparsk_paged_attention(const sparsk_paged_attn_args *a, void *scr
     p.g_inverse = (uint32_t)(((1ull << 32) + p.G - 1) / p.G);
     p.g_limit = p.G == 1 ? 0 : (uint32_t)((1ull << 32) / p.G);  // (by 1 the plain division does)
     p.whole_boxes = PT_WHOLE;
-    p.q_words = aligned(a->q, 4) && a->q_row_stride % 2 == 0 && a->q_head_stride % 2 == 0;
+    p.q_wide = wide(a->q, 2, a->q_row_stride, a->q_head_stride);
     p.out_words = aligned(a->out, 4) && a->out_row_stride % 2 == 0 && a->out_head_stride % 2 == 0;
     int shares = std::min(PT_CTAS * n_sm, PT_MAX_SHARES);
     bool join = true;

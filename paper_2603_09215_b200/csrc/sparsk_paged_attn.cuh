@@ -6,7 +6,7 @@
 // m16n8k16 products (as in sparsk_attn.cuh), so that one read of the head's keys and values serves all of them.
 // All segments, laid end to end in boxes of 16 positions (plus a few boxes' worth for a segment's set-up and end), are cut into equal
 // shares, one for each CTA of a grid that is resident at once: nobody knows the lengths but the device, and
-// every CTA adds them up for itself.  A share begins and ends anywhere; a segment that lies in one share is written
+// one warp of every CTA adds them up.  A share begins and ends anywhere; a segment that lies in one share is written
 // out at once, others leave a partial (sums and maxima) at either end of a share, which
 // a second kernel joins in order.
 //
@@ -27,8 +27,8 @@
 
 namespace sparsk {
 
-constexpr int PT_THREADS = 256, PT_WARPS = 4;  // four warps compute, the fifth brings the boxes, three do nothing: registers
-// are given out by fours of warps, and the four that compute take most of what the others were launched with
+constexpr int PT_THREADS = 256, PT_WARPS = 4, PT_Q_WARPS = 3;  // four warps compute, one brings the boxes, three the queries
+// registers are given out by fours of warps, and the four that compute take most of what the others were launched with
 constexpr int PT_REGS = 200, PT_REGS_BRING = 56; // (times 128 threads each: the launch's 128 times 256)
 constexpr int PT_BOX = 16, PT_STAGE = 64;      // positions
 constexpr int PT_CTAS = 2;                     // resident on an SM
@@ -38,7 +38,7 @@ constexpr int PT_WHOLE = 8;                    // a segment of up to so many box
 constexpr int PT_MIN_SHARE = 28;               // the same unit
 constexpr int PT_C2 = 3, PT_C4 = 6;
 constexpr float PT_LAG = 8.f;                  // in powers of two
-constexpr int PT_RING_BYTES = 112 * 1024;
+constexpr int PT_RING_BYTES = 112 * 1024;      // of a CTA's shared memory: boxes, queries, sums that meet
 constexpr int PJ_THREADS = 256;
 
 // A share's partials for the join: bit 0 its last segment goes on in the next share, bits 1..2 its first one began in an
@@ -68,12 +68,7 @@ struct PtArgs {
     int tiles;          // of 16 query vectors, in a segment at most (1, 2 or 4)
     int whole_boxes;    // segments of up to so many boxes are never cut
     uint32_t g_inverse, g_limit;  // ceil(2^32 / G), and below which numbers it divides by G exactly
-    int q_words, out_words;  // queries and outputs may be read and written two numbers at a time
-};
-
-struct PtFirst {  // the sequence in which a share begins, and where its boxes do
-    long long at;
-    int seq, row0, rows, len;
+    int q_wide, out_words;      // queries may be read sixteen bytes at a time, outputs written two numbers at a time
 };
 
 template <int HD, int CT>
@@ -83,8 +78,10 @@ struct PtForm {
     static constexpr int STAGE = 2 * PT_STAGE * RB;             // keys, then values
     static constexpr int SUMS = PT_WARPS * (HD / 8) * 32 * 16;  // the warps' accumulators
     static constexpr int MEET = SUMS > STAGE ? SUMS - STAGE : 0; // what of them a stage does not hold
-    static constexpr int FIT = (PT_RING_BYTES - MEET) / STAGE, NS = FIT < 12 ? FIT : 12;
-    static constexpr int SMEM = NS * STAGE + MEET + NS * (24 + (int)sizeof(PtStage)) + PT_WARPS * 16 * 8 + PT_THREADS / 4 + (int)sizeof(PtFirst) + 16;
+    static constexpr int QTILE = 16 * HD * 2;                   // a tile's queries
+    static constexpr int FIT = (PT_RING_BYTES - MEET - 4 * QTILE) / STAGE, NS = FIT < 11 ? FIT : 11;
+    static constexpr int SMEM = NS * STAGE + MEET + 4 * QTILE + NS * (16 + (int)sizeof(PtStage)) + 160 + PT_WARPS * 16 * 8 + 16;
+    static_assert(PT_CTAS * (SMEM + 1024) <= 228 * 1024, "two CTAs share an SM");
     // What a box costs where the segment has one tile of vectors (the stage's boxes go to four warps), two (two by two) or more
     // (every box to every warp).
     __host__ __device__ static constexpr int box_cost(int vectors) { return vectors <= 16 ? 2 : vectors <= 32 ? PT_C2 : PT_C4; }
@@ -94,6 +91,8 @@ struct PtForm {
         if (RB == 64) return r * 64 + ((c ^ ((r >> 1) & 3)) << 4);
         return (RB > 128 ? (c >> 3) * (PT_BOX * 128) : 0) + r * 128 + (((c & 7) ^ (r & 7)) << 4);
     }
+    // the same inside a tile of queries
+    __device__ __forceinline__ static int at_q(int r, int c) { return r * HD * 2 + ((c & ~7) << 4) + (((c & 7) ^ (r & 7)) << 4); }
     // at(r, c0 + c) from at(r, c0), c0 below 2 and c even
     __device__ __forceinline__ static int turn(int at0, int c) { return (at0 ^ ((c & 7) << 4)) + (c >> 3) * (PT_BOX * 128); }
 };
@@ -335,12 +334,12 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
     extern __shared__ __align__(1024) unsigned char pt_smem[];
     unsigned char *ring = pt_smem;
     float4 *meet = reinterpret_cast<float4 *>(pt_smem + NS * F::STAGE);
-    uint64_t *full = reinterpret_cast<uint64_t *>(pt_smem + NS * F::STAGE + F::MEET), *empty = full + NS, *told = empty + NS;
-    PtStage *stages = reinterpret_cast<PtStage *>(told + NS);
+    unsigned char *queries = pt_smem + NS * F::STAGE + F::MEET;  // four tiles: of four, two segments or one
+    uint64_t *full = reinterpret_cast<uint64_t *>(queries + 4 * F::QTILE), *empty = full + NS, *q_full = empty + NS, *q_empty = q_full + 4, *q_told = q_empty + 4;
+    int4 *segments = reinterpret_cast<int4 *>(q_told + 4);
+    PtStage *stages = reinterpret_cast<PtStage *>(segments + 4);
     float2 *meet_ml = reinterpret_cast<float2 *>(stages + NS);
-    long long *plan = reinterpret_cast<long long *>(meet_ml + PT_WARPS * 16);  // the warps' sums
-    PtFirst *first = reinterpret_cast<PtFirst *>(plan + PT_THREADS / 32);
-    uint64_t *meeting = reinterpret_cast<uint64_t *>(first + 1);
+    uint64_t *meeting = reinterpret_cast<uint64_t *>(meet_ml + PT_WARPS * 16);
     volatile int *giving_up = reinterpret_cast<volatile int *>(meeting + 1);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
@@ -353,77 +352,127 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
         for (int s = 0; s < NS; s++) {
             mbar_init(&full[s], 1);
             mbar_init(&empty[s], PT_WARPS);
-            mbar_init(&told[s], 1);
+        }
+        for (int s = 0; s < 4; s++) {
+            mbar_init(&q_full[s], PT_Q_WARPS * 32);
+            mbar_init(&q_empty[s], PT_WARPS);
+            mbar_init(&q_told[s], 1);
         }
         mbar_init(meeting, PT_WARPS);
         giving_up[0] = giving_up[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    __syncthreads();
     griddep_wait();
 
     // What the boxes' addresses and the queries wait for, on its way to the L2 while the lengths are added up: every CTA
     // asks for its part of the tables (as far as that is a few lines a thread).
-    {
+    if (warp < PT_WARPS) {
         const int lines = (a.max_blocks + 31) / 32;
-        const long long all = (long long)lines * a.n_seqs, n_thr = (long long)gridDim.x * PT_THREADS;
-        if (all <= 4 * n_thr)
-            for (long long i = (long long)blockIdx.x * PT_THREADS + tid; i < all; i += n_thr) prefetch_l2(a.block_table + (i / lines) * a.table_stride + i % lines * 32);
+        const unsigned n_thr = gridDim.x * PT_WARPS * 32;
+        if ((long long)lines * a.n_seqs <= 4 * n_thr)
+            for (unsigned i = blockIdx.x * PT_WARPS * 32 + tid; i < (unsigned)(lines * a.n_seqs); i += n_thr)
+                prefetch_l2(a.block_table + (long long)(i / lines) * a.table_stride + i % lines * 32);
     }
-    // this CTA's share [beg, end) of all segments' boxes
     const int cap = a.max_blocks * a.page_size;
-    const auto boxes_of = [&](const PtSeq &s) { return (min(s.len, cap) + PT_BOX - 1) / PT_BOX; };
-    const auto box_cost = [&](const PtSeq &s) { return F::box_cost((int)min((long long)s.rows * a.G, a.tiles * 16LL)); };
-    const auto cost_of = [&](const PtSeq &s) { return boxes_of(s) * box_cost(s) + PT_END_COST; };
-    const int per = (a.n_seqs + PT_THREADS - 1) / PT_THREADS, s_beg = min(tid * per, a.n_seqs), s_end = min(s_beg + per, a.n_seqs);
-    long long mine = 0;
-    PtSeq s{};
-    for (int i = s_beg; i < s_end; i++) {
-        s = pt_seq(a, i);
-        mine += pt_segments(a, s.rows) * cost_of(s);
-    }
-    long long upto = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long y = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += y;
-    }
-    if (lane == 31) plan[warp] = upto;
-    __syncthreads();
-    long long total = 0;
-#pragma unroll
-    for (int w = 0; w < PT_THREADS / 32; w++) {
-        if (w < warp) upto += plan[w];
-        total += plan[w];
-    }
-    const long long share = max(pt_div(total + gridDim.x - 1, gridDim.x), (long long)PT_MIN_SHARE);
-    const long long beg = share * blockIdx.x, end = min(beg + share, total);
-    if (beg >= end) {
-        if (tid == 0) a.records[blockIdx.x].flags = 0;
-        return;
-    }
-    if (mine > 0 && upto - mine <= beg && beg < upto) {  // the sequence in which it begins is one of this thread's
-        long long at = upto - mine;
-        int i = s_beg;
-        if (per > 1)
-            for (;; i++) {
-                s = pt_seq(a, i);
-                const long long c = pt_segments(a, s.rows) * cost_of(s);
-                if (beg < at + c) break;
-                at += c;
-            }
-        *first = PtFirst{at, i, s.row0, s.rows, s.len};
-    }
-    __syncthreads();
-
+    const int q_shift = a.tiles == 1 ? 2 : a.tiles == 2 ? 1 : 0, q_slots = 1 << q_shift;
     if (warp >= PT_WARPS) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PT_REGS_BRING));
-        if (warp > PT_WARPS) return;
+        if (warp > PT_WARPS) {
+            // ------------------------------------------------------------ the warps that bring the queries, sixteen bytes a lane
+            // and copy.  (Read by the computing warps themselves, as the lanes hold them, they cost four times the sectors in each of
+            // four warps and a trip to the memory at every segment's start.)
+            for (int segs = 0;; segs++) {
+                const int slot = segs & (q_slots - 1);
+                if (!pt_wait(&q_told[slot], (segs >> q_shift) & 1, giving_up)) break;
+                const int4 seg = segments[slot];  // first row, rows, block of vectors, kv head
+                if (seg.y < 0) break;
+                const int v_first = seg.z * a.tiles * 16, n_here = min(seg.y * a.G - v_first, a.tiles * 16);
+                unsigned char *dst = queries + slot * a.tiles * F::QTILE;
+                for (int i = tid - (PT_WARPS + 1) * 32; i < n_here * (HD / 8); i += PT_Q_WARPS * 32) {
+                    const int v = i / (HD / 8), c = i % (HD / 8), r = pt_row_of(a, v_first + v);
+                    const uint16_t *src = reinterpret_cast<const uint16_t *>(a.q) + (seg.x + r) * a.q_row_stride +
+                                          (seg.w * a.G + v_first + v - r * a.G) * a.q_head_stride + c * 8;
+                    unsigned char *to_q = dst + F::at_q(v, c);
+                    if (a.q_wide) cp_async16(to_q, src, 16);
+                    else {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int k = 0; k < 4; k++) w[k] = (uint32_t)src[2 * k] | ((uint32_t)src[2 * k + 1] << 16);
+                        *reinterpret_cast<uint4 *>(to_q) = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                }
+                if (a.q_wide) asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&q_full[slot])) : "memory");
+                else mbar_arrive(&q_full[slot]);
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            return;
+        }
         // ---------------------------------------------------------------- the warp that brings the boxes
-        int seq = first->seq, base = seq, it = 0, issued = 0, flags = 0;
-        long long at = first->at, x = beg;
-        PtSeq now{first->row0, first->rows, first->len};
+        // First its share [beg, end) of all segments' boxes: 256 sequences at a time, up to eight a lane.
+        const auto boxes_of = [&](const PtSeq &s) { return (min(s.len, cap) + PT_BOX - 1) / PT_BOX; };
+        const auto box_cost = [&](const PtSeq &s) { return F::box_cost((int)min((long long)s.rows * a.G, a.tiles * 16LL)); };
+        const auto cost_of = [&](const PtSeq &s) { return boxes_of(s) * box_cost(s) + PT_END_COST; };
+        const int per = min((a.n_seqs + 31) / 32, 8);
         PtSeq ahead{};  // of sequence base + lane
-        if (seq + lane < a.n_seqs) ahead = pt_seq(a, seq + lane);
+        long long costs[8], mine, upto;
+        const auto add_up = [&](int s0) {  // of the sequences from s0
+            mine = 0;
+#pragma unroll
+            for (int k = 0; k < 8; k++) {
+                const int i = s0 + lane * per + k;
+                costs[k] = 0;
+                if (k < per && i < a.n_seqs) {
+                    const PtSeq s = pt_seq(a, i);
+                    if (per == 1) ahead = s;
+                    costs[k] = pt_segments(a, s.rows) * cost_of(s);
+                }
+                mine += costs[k];
+            }
+            upto = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long y = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += y;
+            }
+            return __shfl_sync(0xffffffffu, upto, 31);
+        };
+        long long total = 0;
+        for (int s0 = 0; s0 < a.n_seqs; s0 += 32 * per) total += add_up(s0);
+        const long long share = max(pt_div(total + gridDim.x - 1, gridDim.x), (long long)PT_MIN_SHARE);
+        const long long beg = share * blockIdx.x, end = min(beg + share, total);
+        int seq = 0, base = 0, it = 0, issued = 0, flags = 0, segs = 0;
+        long long at = 0, x = beg;
+        PtSeq now{};
+        if (beg < end) {
+            // the sequence in which it begins
+            for (int s0 = 0;; s0 += 32 * per) {
+                const long long all = a.n_seqs > 32 * per ? add_up(s0) : total;
+                if (beg < at + all) {
+                    const uint32_t b = __ballot_sync(0xffffffffu, beg < at + upto);
+                    const int from = __ffs(b) - 1;
+                    long long c = at + upto - mine;
+                    int k0 = 0;
+#pragma unroll
+                    for (int k = 0; k < 7; k++)
+                        if (k0 == k && k + 1 < per && beg >= c + costs[k]) {
+                            c += costs[k];
+                            k0++;
+                        }
+                    at = __shfl_sync(0xffffffffu, c, from);
+                    seq = s0 + from * per + __shfl_sync(0xffffffffu, k0, from);
+                    break;
+                }
+                at += all;
+            }
+            if (per > 1) {
+                base = seq;
+                if (seq + lane < a.n_seqs) ahead = pt_seq(a, seq + lane);
+            }
+            now.row0 = __shfl_sync(0xffffffffu, ahead.row0, seq - base);
+            now.rows = __shfl_sync(0xffffffffu, ahead.rows, seq - base);
+            now.len = __shfl_sync(0xffffffffu, ahead.len, seq - base);
+        }
         PtRecord rec{};
         bool ok = true;
         const auto next_stage = [&]() {
@@ -472,12 +521,15 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
                 rec.qblk = qblk;
                 rec.head = head;
             }
-            // the queries on their way to the L2, behind which a whole stage's copies would have to wait
-            const int n_here = min(now.rows * a.G - qblk * a.tiles * 16, a.tiles * 16);
-            for (int i = lane; i < n_here * (HD / 64); i += 32) {
-                const int v = qblk * a.tiles * 16 + i / (HD / 64), r = pt_row_of(a, v);
-                prefetch_l2(reinterpret_cast<const uint16_t *>(a.q) + (now.row0 + r) * a.q_row_stride +
-                            (head * a.G + v - r * a.G) * a.q_head_stride + i % (HD / 64) * 64);
+            {
+                const int slot = segs & (q_slots - 1);
+                if (segs >= q_slots) ok = ok && pt_wait(&q_empty[slot], ((segs >> q_shift) - 1) & 1, giving_up);
+                if (!ok) break;
+                segs++;
+                if (lane == 0) {
+                    segments[slot] = make_int4(now.row0, now.rows, qblk, head);
+                    mbar_arrive(&q_told[slot]);
+                }
             }
             const int pos_end = min(min(now.len, cap), b1 * PT_BOX);
             int page = -1;
@@ -505,7 +557,6 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
                     d.len = now.len;
                     d.qblk = qblk;
                     d.head = head;
-                    mbar_arrive(&told[st]);
                     mbar_expect_tx(&full[st], (uint32_t)__popc(have) * 2u * PT_BOX * RB);
                 }
                 __syncwarp();
@@ -517,11 +568,15 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
                 issued = it;
             }
         }
+        if (ok && segs >= q_slots) ok = pt_wait(&q_empty[segs & (q_slots - 1)], ((segs >> q_shift) - 1) & 1, giving_up);
+        if (ok && lane == 0) {
+            segments[segs & (q_slots - 1)].y = -1;
+            mbar_arrive(&q_told[segs & (q_slots - 1)]);
+        }
         if (ok) {
             const int st = next_stage();
             if (lane == 0 && ok) {
                 stages[st].flags = PT_STOP;
-                mbar_arrive(&told[st]);
                 mbar_arrive(&full[st]);
             }
         }
@@ -543,7 +598,7 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
     float o[NT][4], m_run[2], l_run[2], c_log2 = 0.f;
     // where this lane reads its rows of a box: the chunk's low bit is the lane's, even steps turn the others
     const int k_at = F::at((lane & 7) + ((lane >> 4) << 3), (lane >> 3) & 1), v_at = F::at((lane & 7) + ((lane >> 3) & 1) * 8, lane >> 4);
-    int limit[2], lim_min = 0, meetings = 0;
+    int limit[2], lim_min = 0, meetings = 0, segs = 0;
     // all four warps; like every wait here it ends by itself when another warp has given up
     const auto meet_here = [&]() {
         __syncwarp();
@@ -552,8 +607,7 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
     };
     for (int it = 0;; it++) {
         const int st = it % NS;
-        // what the stage holds is known before it has come: a new segment's queries are asked for meanwhile
-        if (!pt_wait(&told[st], (it / NS) & 1, giving_up)) return;
+        if (!pt_wait(&full[st], (it / NS) & 1, giving_up)) return;
         const PtStage d = stages[st];
         if (d.flags & PT_STOP) break;
         const int n_vec = d.rows * a.G;  // of the sequence
@@ -575,35 +629,31 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
             for (int hf = 0; hf < 2; hf++) {
                 const int v = v0 + (lane >> 2) + hf * 8;
                 const bool have = v < n_vec;
-                const int r = have ? pt_row_of(a, v) : 0, h = have ? v - r * a.G : 0;
                 m_run[hf] = -INFINITY;
                 l_run[hf] = 0.f;
-                limit[hf] = have ? d.len - d.rows + r : -1;  // the last position that this vector sees
-                // (a tile's missing vectors compute with the sequence's first one, and nobody reads it)
-                const uint16_t *q = reinterpret_cast<const uint16_t *>(a.q) + (d.row0 + r) * a.q_row_stride + (d.head * a.G + h) * a.q_head_stride;
-                // 8-bit keys come four dimensions to a lane, 16-bit keys two and two
-                constexpr int STEP = F::ES == 1 ? 4 : 2, NEXT = F::ES == 1 ? 2 : 8;
-                if (a.q_words) {
-#pragma unroll
-                    for (int ks = 0; ks < KS; ks++) {
-                        qa[ks][hf] = *reinterpret_cast<const uint32_t *>(q + ks * 16 + t4 * STEP);
-                        qa[ks][2 + hf] = *reinterpret_cast<const uint32_t *>(q + ks * 16 + t4 * STEP + NEXT);
-                    }
-                } else {
-#pragma unroll
-                    for (int ks = 0; ks < KS; ks++) {
-                        const uint16_t *x = q + ks * 16 + t4 * STEP;
-                        qa[ks][hf] = (uint32_t)x[0] | ((uint32_t)x[1] << 16);
-                        qa[ks][2 + hf] = (uint32_t)x[NEXT] | ((uint32_t)x[NEXT + 1] << 16);
-                    }
-                }
+                limit[hf] = have ? d.len - d.rows + pt_row_of(a, v) : -1;  // the last position that this vector sees
             }
+            // (the rows of vectors that a tile does not have hold anything, and nobody reads what comes of them)
+            const int slot = segs & (q_slots - 1);
+            if (!pt_wait(&q_full[slot], (segs >> q_shift) & 1, giving_up)) return;
+            segs++;
+            const unsigned char *Q = queries + (slot * a.tiles + mt) * F::QTILE;
+#pragma unroll
+            for (int ks = 0; ks < KS; ks++) {
+                if constexpr (F::ES == 1) {
+                    // 8-bit keys come four dimensions to a lane
+                    const uint2 x = *reinterpret_cast<const uint2 *>(Q + F::at_q(lane >> 2, ks * 2 + (t4 >> 1)) + (t4 & 1) * 8);
+                    const uint2 y = *reinterpret_cast<const uint2 *>(Q + F::at_q((lane >> 2) + 8, ks * 2 + (t4 >> 1)) + (t4 & 1) * 8);
+                    qa[ks][0] = x.x; qa[ks][1] = y.x; qa[ks][2] = x.y; qa[ks][3] = y.y;
+                } else ldsm_x4(qa[ks], Q + F::at_q(lane & 15, ks * 2 + (lane >> 4)));
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&q_empty[slot]);
 #pragma unroll
             for (int ks = 0; ks < KS; ks++)
 #pragma unroll
                 for (int i = 0; i < 4; i++) qa[ks][i] = pt_query2<CT>(qa[ks][i], a.q_type);
         }
-        if (!pt_wait(&full[st], (it / NS) & 1, giving_up)) return;
         bool wrote = false;
 #pragma unroll 1
         for (int b = v0 < n_vec ? pg : 4; b < 4; b += PG) {  // (a tile without vectors has nothing to do)
@@ -704,99 +754,105 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
         }
 
         // ---------------------------------------------------------------- the piece's end
-        float l[2], m[2] = {m_run[0], m_run[1]};
-#pragma unroll
-        for (int hf = 0; hf < 2; hf++) {
-            l[hf] = l_run[hf];
-            l[hf] += __shfl_xor_sync(0xffffffffu, l[hf], 1);
-            l[hf] += __shfl_xor_sync(0xffffffffu, l[hf], 2);
-        }
-        if (PG > 1) {
-            // the warps of one block of vectors: to a common maximum
-            if (t4 == 0) {
-                meet_ml[warp * 16 + (lane >> 2)] = make_float2(m[0], l[0]);
-                meet_ml[warp * 16 + (lane >> 2) + 8] = make_float2(m[1], l[1]);
-            }
-            if (!meet_here()) return;
+        const auto finish = [&](auto warps) {
+            constexpr int W = decltype(warps)::value;  // of the tile
+            const bool part = d.flags & (PT_HEAD_PART | PT_TAIL_PART);
+            const size_t cell = ((size_t)blockIdx.x * 2 + (d.flags & PT_TAIL_PART ? 1 : 0)) * a.tiles + mt;
+            const float vs = a.v_scale ? a.v_scale[d.head] : 1.f;
+            float l[2], m[2] = {m_run[0], m_run[1]}, inv[2];
+            long long to[2];
+            bool have[2];
 #pragma unroll
             for (int hf = 0; hf < 2; hf++) {
-                float top = -INFINITY, sum = 0.f;
-                for (int g = 0; g < PG; g++) top = fmaxf(top, meet_ml[(warp + (g - pg) * (PT_WARPS / PG)) * 16 + (lane >> 2) + hf * 8].x);
-                const float use = top == -INFINITY ? 0.f : top;
-                for (int g = 0; g < PG; g++) {
-                    const float2 x = meet_ml[(warp + (g - pg) * (PT_WARPS / PG)) * 16 + (lane >> 2) + hf * 8];
-                    sum += x.y * exp2f(x.x - use);
-                }
-                const float f = exp2f(m[hf] - use);
-                if (f != 1.f) {
+                l[hf] = l_run[hf];
+                l[hf] += __shfl_xor_sync(0xffffffffu, l[hf], 1);
+                l[hf] += __shfl_xor_sync(0xffffffffu, l[hf], 2);
+                if (W > 1 && t4 == 0) meet_ml[warp * 16 + (lane >> 2) + hf * 8] = make_float2(m[hf], l[hf]);
+                const int v = v0 + (lane >> 2) + hf * 8, r = pt_row_of(a, v), h = d.head * a.G + v - r * a.G;
+                have[hf] = v < n_vec;
+                to[hf] = (d.row0 + r) * a.out_row_stride + h * a.out_head_stride;
+            }
+            if (W > 1) {
+                // to a common maximum (and everybody has read the stage)
+                if (!meet_here()) return false;
+                float2 ml[2][W];
+#pragma unroll
+                for (int hf = 0; hf < 2; hf++)
+#pragma unroll
+                    for (int g = 0; g < W; g++) ml[hf][g] = meet_ml[(mt + g * (PT_WARPS / W)) * 16 + (lane >> 2) + hf * 8];
+#pragma unroll
+                for (int hf = 0; hf < 2; hf++) {
+                    float top = ml[hf][0].x, sum = 0.f;
+#pragma unroll
+                    for (int g = 1; g < W; g++) top = fmaxf(top, ml[hf][g].x);
+                    const float use = top == -INFINITY ? 0.f : top;
+#pragma unroll
+                    for (int g = 0; g < W; g++) sum += ml[hf][g].y * exp2f(ml[hf][g].x - use);
+                    const float f = exp2f(m[hf] - use);
 #pragma unroll
                     for (int nt = 0; nt < NT; nt++) {
                         o[nt][hf * 2] *= f;
                         o[nt][hf * 2 + 1] *= f;
                     }
+                    m[hf] = top;
+                    l[hf] = sum;
                 }
-                m[hf] = top;
-                l[hf] = sum;
             }
-        }
-        const bool part = d.flags & (PT_HEAD_PART | PT_TAIL_PART);
-        const size_t cell = ((size_t)blockIdx.x * 2 + (d.flags & PT_TAIL_PART ? 1 : 0)) * a.tiles + mt;
-        float inv[2];
-        long long to[2];
-        bool have[2];
-        const float vs = a.v_scale ? a.v_scale[d.head] : 1.f;
+            // the tile's warps add their sums up in the stage that they have just read (and held back)
+            const auto sums = [&](int w, int nt) {
+                const int i = (w * NT + nt) * 32 + lane;
+                return F::MEET && i >= F::STAGE / 16 ? meet + (i - F::STAGE / 16) : reinterpret_cast<float4 *>(ring + st * F::STAGE) + i;
+            };
+            if (W > 1) {
 #pragma unroll
-        for (int hf = 0; hf < 2; hf++) {
-            const int v = v0 + (lane >> 2) + hf * 8;
-            have[hf] = v < n_vec;
-            const int r = have[hf] ? pt_row_of(a, v) : 0, h = d.head * a.G + (have[hf] ? v - r * a.G : 0);
-            to[hf] = (d.row0 + r) * a.out_row_stride + h * a.out_head_stride;
-            inv[hf] = l[hf] == 0.f ? 0.f : __fdividef(vs, l[hf]);
-            if (t4 == 0 && pg == 0) {
-                if (part) a.part_ml[cell * 16 + (lane >> 2) + hf * 8] = make_float2(m[hf], l[hf]);
-                else if (a.lse && have[hf]) a.lse[(long long)(d.row0 + r) * a.Hk * a.G + h] = l[hf] == 0.f ? -INFINITY : (m[hf] + log2f(l[hf])) * LN2;
+                for (int nt = 0; nt < NT; nt++) *sums(warp, nt) = make_float4(o[nt][0], o[nt][1], o[nt][2], o[nt][3]);
+            } else release();
+#pragma unroll
+            for (int hf = 0; hf < 2; hf++) {
+                inv[hf] = l[hf] == 0.f ? 0.f : __fdividef(vs, l[hf]);
+                if (t4 == 0 && pg == 0) {
+                    if (part) a.part_ml[cell * 16 + (lane >> 2) + hf * 8] = make_float2(m[hf], l[hf]);
+                    else if (a.lse && have[hf]) {
+                        const int v = v0 + (lane >> 2) + hf * 8, r = pt_row_of(a, v);
+                        a.lse[(long long)(d.row0 + r) * a.Hk * a.G + d.head * a.G + v - r * a.G] = l[hf] == 0.f ? -INFINITY : (m[hf] + log2f(l[hf])) * LN2;
+                    }
+                }
             }
-        }
-        // Accumulators x0 and x1 of products nt and nt + 1, as a partial or as outputs.
-        const auto put = [&](int nt, const float4 &x0, const float4 &x1) {
-            if (part) {
-                a.part_o[(cell * NT + nt) * 32 + lane] = x0;
-                a.part_o[(cell * NT + nt + 1) * 32 + lane] = x1;
-            } else {
-                if (have[0]) pt_put<F::ES>(a, to[0], nt, t4, x0.x * inv[0], x0.y * inv[0], x1.x * inv[0], x1.y * inv[0]);
-                if (have[1]) pt_put<F::ES>(a, to[1], nt, t4, x0.z * inv[1], x0.w * inv[1], x1.z * inv[1], x1.w * inv[1]);
-            }
-        };
-        if (PG == 1) {
-            release();
+            if (W > 1 && !meet_here()) return false;
+            // every warp its share of the dimensions, two neighbouring products at a time
 #pragma unroll
-            for (int nt = 0; nt < NT; nt += 2)
-                put(nt, make_float4(o[nt][0], o[nt][1], o[nt][2], o[nt][3]), make_float4(o[nt + 1][0], o[nt + 1][1], o[nt + 1][2], o[nt + 1][3]));
-            continue;
-        }
-        // the tile's warps add their sums up in the stage that they have just read (and held back)
-        const auto sums = [&](int w, int nt) {
-            const int i = (w * NT + nt) * 32 + lane;
-            return F::MEET && i >= F::STAGE / 16 ? meet + (i - F::STAGE / 16) : reinterpret_cast<float4 *>(ring + st * F::STAGE) + i;
-        };
-#pragma unroll
-        for (int nt = 0; nt < NT; nt++) *sums(warp, nt) = make_float4(o[nt][0], o[nt][1], o[nt][2], o[nt][3]);
-        if (!meet_here()) return;
-#pragma unroll 1
-        for (int nt = pg * 2; nt < NT; nt += PG * 2) {
-            float4 x[2] = {*sums(mt, nt), *sums(mt, nt + 1)};
-#pragma unroll 1
-            for (int w = mt + PT_WARPS / PG; w < PT_WARPS; w += PT_WARPS / PG) {
+            for (int j = 0; j < NT / 2 / W; j++) {
+                const int nt = (j * W + pg) * 2;
+                float4 x[2];
 #pragma unroll
                 for (int k = 0; k < 2; k++) {
-                    const float4 y = *sums(w, nt + k);
-                    x[k].x += y.x; x[k].y += y.y; x[k].z += y.z; x[k].w += y.w;
+                    if (W == 1) x[k] = make_float4(o[j * 2 + k][0], o[j * 2 + k][1], o[j * 2 + k][2], o[j * 2 + k][3]);
+                    else x[k] = *sums(mt, nt + k);
+#pragma unroll
+                    for (int g = 1; g < W; g++) {
+                        const float4 y = *sums(mt + g * (PT_WARPS / W), nt + k);
+                        x[k].x += y.x; x[k].y += y.y; x[k].z += y.z; x[k].w += y.w;
+                    }
+                }
+                if (part) {
+                    a.part_o[(cell * NT + nt) * 32 + lane] = x[0];
+                    a.part_o[(cell * NT + nt + 1) * 32 + lane] = x[1];
+                } else {
+                    if (have[0]) pt_put<F::ES>(a, to[0], nt, t4, x[0].x * inv[0], x[0].y * inv[0], x[1].x * inv[0], x[1].y * inv[0]);
+                    if (have[1]) pt_put<F::ES>(a, to[1], nt, t4, x[0].z * inv[1], x[0].w * inv[1], x[1].z * inv[1], x[1].w * inv[1]);
                 }
             }
-            put(nt, x[0], x[1]);
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        release();
+            if (W > 1) {
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                release();
+            }
+            return true;
+        };
+        if (PG == 4) {
+            if (!finish(std::integral_constant<int, 4>{})) return;
+        } else if (PG == 2) {
+            if (!finish(std::integral_constant<int, 2>{})) return;
+        } else finish(std::integral_constant<int, 1>{});
     }
 }
 
