@@ -66,7 +66,7 @@ bool paged_attn_ok(const sparsk_paged_attn_args *a)
     if (a->max_rows < 0 || a->max_len < 0 || (!a->row_start && a->n_rows != a->n_seqs)) return false;
     if (!(a->scale >= 0.f) || !(a->scale < INFINITY)) return false;
     if (a->table_stride < a->max_blocks || a->table_stride > INT_MAX) return false;
-    if ((int64_t)a->max_blocks * a->pool.page_size > INT_MAX) return false;
+    if ((int64_t)a->max_blocks * a->pool.page_size > INT_MAX || (int64_t)a->n_rows * a->n_q_heads > INT_MAX / 2) return false;
     return strides_ok(a->q_row_stride, a->q_head_stride) && strides_ok(a->out_row_stride, a->out_head_stride);
 }
 
@@ -166,6 +166,9 @@ extern "C" int sparsk_paged_attention(const sparsk_paged_attn_args *a, void *scr
     p.g_inverse = (uint32_t)(((1ull << 32) + p.G - 1) / p.G);
     p.g_limit = p.G == 1 ? 0 : (uint32_t)((1ull << 32) / p.G);  // (by 1 the plain division does)
     p.whole_boxes = PT_WHOLE;
+    p.page_shift = -1;
+    for (int i = 0; i < 28; i++)
+        if (p.page_size == PT_BOX << i) p.page_shift = i;
     p.q_wide = wide(a->q, 2, a->q_row_stride, a->q_head_stride);
     p.out_words = aligned(a->out, 4) && a->out_row_stride % 2 == 0 && a->out_head_stride % 2 == 0;
     int shares = std::min(PT_CTAS * n_sm, PT_MAX_SHARES);

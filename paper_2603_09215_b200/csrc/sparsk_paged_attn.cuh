@@ -66,6 +66,7 @@ struct PtArgs {
     float scale_log2;
     int q_type, n_rows, n_seqs, max_blocks, page_size, n_pages, Hk, G;
     int tiles;          // of 16 query vectors, in a segment at most (1, 2 or 4)
+    int page_shift;     // a page has 2^page_shift boxes, or -1
     int whole_boxes;    // segments of up to so many boxes are never cut
     uint32_t g_inverse, g_limit;  // ceil(2^32 / G), and below which numbers it divides by G exactly
     int q_wide, out_words;      // queries may be read sixteen bytes at a time, outputs written two numbers at a time
@@ -84,7 +85,7 @@ struct PtForm {
     static_assert(PT_CTAS * (SMEM + 1024) <= 228 * 1024, "two CTAs share an SM");
     // What a box costs where the segment has one tile of vectors (the stage's boxes go to four warps), two (two by two) or more
     // (every box to every warp).
-    __host__ __device__ static constexpr int box_cost(int vectors) { return vectors <= 16 ? 2 : vectors <= 32 ? PT_C2 : PT_C4; }
+    __device__ __forceinline__ static int box_cost(int vectors) { return vectors <= 16 ? 2 : vectors <= 32 ? PT_C2 : PT_C4; }
     // byte offset of 16-byte chunk c of row r inside a box
     __device__ __forceinline__ static int at(int r, int c)
     {
@@ -262,15 +263,16 @@ __device__ __forceinline__ PtSeq pt_seq(const PtArgs &a, int i)
     return s;
 }
 // segments of a sequence
-__device__ __forceinline__ long long pt_segments(const PtArgs &a, int rows)
+__device__ __forceinline__ int pt_segments(const PtArgs &a, int rows)
 {
     const int shift = a.tiles == 1 ? 4 : a.tiles == 2 ? 5 : 6;
-    return (((long long)rows * a.G + (1 << shift) - 1) >> shift) * a.Hk;
+    return ((rows * a.G + (1 << shift) - 1) >> shift) * a.Hk;  // (rows times query heads fit 31 bits)
 }
-// x / y for x >= 0, y > 0; almost always of 32 bits, which divide several times as fast
+// x / y for x >= 0, y > 0: almost always of 32 bits, which divide several times as fast
+static __device__ __noinline__ long long pt_div_wide(long long x, int y) { return x / y; }
 __device__ __forceinline__ long long pt_div(long long x, int y)
 {
-    return (x >> 32) == 0 ? (long long)((unsigned)x / (unsigned)y) : x / y;
+    return (x >> 32) == 0 ? (long long)((unsigned)x / (unsigned)y) : pt_div_wide(x, y);
 }
 // v / G for a query vector's number
 __device__ __forceinline__ int pt_row_of(const PtArgs &a, int v)
@@ -362,19 +364,34 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
         giving_up[0] = giving_up[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    __syncthreads();
     griddep_wait();
 
-    // What the boxes' addresses and the queries wait for, on its way to the L2 while the lengths are added up: every CTA
-    // asks for its part of the tables (as far as that is a few lines a thread).
-    if (warp < PT_WARPS) {
-        const int lines = (a.max_blocks + 31) / 32;
-        const unsigned n_thr = gridDim.x * PT_WARPS * 32;
-        if ((long long)lines * a.n_seqs <= 4 * n_thr)
-            for (unsigned i = blockIdx.x * PT_WARPS * 32 + tid; i < (unsigned)(lines * a.n_seqs); i += n_thr)
-                prefetch_l2(a.block_table + (long long)(i / lines) * a.table_stride + i % lines * 32);
-    }
+    // This CTA's share [beg, end) of all segments' boxes.  What a thread's sequences cost, and what those before them do:
     const int cap = a.max_blocks * a.page_size;
+    const auto boxes_of = [&](const PtSeq &s) { return (min(s.len, cap) + PT_BOX - 1) / PT_BOX; };
+    const auto box_cost = [&](const PtSeq &s) { return F::box_cost(min(s.rows * a.G, a.tiles * 16)); };
+    const auto cost_of = [&](const PtSeq &s) { return boxes_of(s) * box_cost(s) + PT_END_COST; };
+    const int per = (a.n_seqs + PT_THREADS - 1) / PT_THREADS;
+    long long *plan = reinterpret_cast<long long *>(queries);           // [256]: up to and with a thread's sequences, in its warp
+    PtSeq *plan_seq = reinterpret_cast<PtSeq *>(plan + PT_THREADS);     // [256], where a thread has one sequence
+    {
+        long long mine = 0;
+#pragma unroll 1
+        for (int i = tid * per; i < min((tid + 1) * per, a.n_seqs); i++) {
+            // (the lines of the tables on their way to the L2 meanwhile, one for each CTA)
+            if ((int)blockIdx.x * 32 < a.max_blocks) prefetch_l2(a.block_table + i * a.table_stride + blockIdx.x * 32);
+            const PtSeq s = pt_seq(a, i);
+            mine += (long long)pt_segments(a, s.rows) * cost_of(s);
+            plan_seq[tid] = s;
+        }
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, mine, o);
+            if (lane >= o) mine += y;
+        }
+        plan[tid] = mine;
+    }
+    __syncthreads();
     const int q_shift = a.tiles == 1 ? 2 : a.tiles == 2 ? 1 : 0, q_slots = 1 << q_shift;
     if (warp >= PT_WARPS) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PT_REGS_BRING));
@@ -409,69 +426,33 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
             return;
         }
         // ---------------------------------------------------------------- the warp that brings the boxes
-        // First its share [beg, end) of all segments' boxes: 256 sequences at a time, up to eight a lane.
-        const auto boxes_of = [&](const PtSeq &s) { return (min(s.len, cap) + PT_BOX - 1) / PT_BOX; };
-        const auto box_cost = [&](const PtSeq &s) { return F::box_cost((int)min((long long)s.rows * a.G, a.tiles * 16LL)); };
-        const auto cost_of = [&](const PtSeq &s) { return boxes_of(s) * box_cost(s) + PT_END_COST; };
-        const int per = min((a.n_seqs + 31) / 32, 8);
-        PtSeq ahead{};  // of sequence base + lane
-        long long costs[8], mine, upto;
-        const auto add_up = [&](int s0) {  // of the sequences from s0
-            mine = 0;
+        long long upto = lane < PT_THREADS / 32 ? plan[lane * 32 + 31] : 0;
 #pragma unroll
-            for (int k = 0; k < 8; k++) {
-                const int i = s0 + lane * per + k;
-                costs[k] = 0;
-                if (k < per && i < a.n_seqs) {
-                    const PtSeq s = pt_seq(a, i);
-                    if (per == 1) ahead = s;
-                    costs[k] = pt_segments(a, s.rows) * cost_of(s);
-                }
-                mine += costs[k];
-            }
-            upto = mine;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const long long y = __shfl_up_sync(0xffffffffu, upto, o);
-                if (lane >= o) upto += y;
-            }
-            return __shfl_sync(0xffffffffu, upto, 31);
-        };
-        long long total = 0;
-        for (int s0 = 0; s0 < a.n_seqs; s0 += 32 * per) total += add_up(s0);
+        for (int o = 1; o < PT_THREADS / 32; o <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += y;
+        }
+        const long long total = __shfl_sync(0xffffffffu, upto, PT_THREADS / 32 - 1);
         const long long share = max(pt_div(total + gridDim.x - 1, gridDim.x), (long long)PT_MIN_SHARE);
         const long long beg = share * blockIdx.x, end = min(beg + share, total);
         int seq = 0, base = 0, it = 0, issued = 0, flags = 0, segs = 0;
         long long at = 0, x = beg;
-        PtSeq now{};
+        PtSeq now{}, ahead{};  // `ahead`: of sequence base + lane
         if (beg < end) {
-            // the sequence in which it begins
-            for (int s0 = 0;; s0 += 32 * per) {
-                const long long all = a.n_seqs > 32 * per ? add_up(s0) : total;
-                if (beg < at + all) {
-                    const uint32_t b = __ballot_sync(0xffffffffu, beg < at + upto);
-                    const int from = __ffs(b) - 1;
-                    long long c = at + upto - mine;
-                    int k0 = 0;
-#pragma unroll
-                    for (int k = 0; k < 7; k++)
-                        if (k0 == k && k + 1 < per && beg >= c + costs[k]) {
-                            c += costs[k];
-                            k0++;
-                        }
-                    at = __shfl_sync(0xffffffffu, c, from);
-                    seq = s0 + from * per + __shfl_sync(0xffffffffu, k0, from);
-                    break;
-                }
-                at += all;
-            }
-            if (per > 1) {
-                base = seq;
-                if (seq + lane < a.n_seqs) ahead = pt_seq(a, seq + lane);
-            }
-            now.row0 = __shfl_sync(0xffffffffu, ahead.row0, seq - base);
-            now.rows = __shfl_sync(0xffffffffu, ahead.rows, seq - base);
-            now.len = __shfl_sync(0xffffffffu, ahead.len, seq - base);
+            // the sequence in which it begins: its warp, its thread, and of a thread's sequences which
+            const int w = __ffs(__ballot_sync(0xffffffffu, beg < upto && lane < PT_THREADS / 32)) - 1;
+            const long long before = w > 0 ? __shfl_sync(0xffffffffu, upto, w - 1) : 0, in_warp = plan[w * 32 + lane];
+            const int l = __ffs(__ballot_sync(0xffffffffu, beg < before + in_warp)) - 1;
+            const long long before_lane = __shfl_sync(0xffffffffu, in_warp, max(l - 1, 0));
+            at = before + (l > 0 ? before_lane : 0);
+            seq = base = (w * 32 + l) * per;
+            if (per == 1) {
+                if (seq + lane < a.n_seqs) ahead = plan_seq[seq + lane];
+            } else if (seq + lane < a.n_seqs) ahead = pt_seq(a, seq + lane);
+            now.row0 = __shfl_sync(0xffffffffu, ahead.row0, 0);
+            now.rows = __shfl_sync(0xffffffffu, ahead.rows, 0);
+            now.len = __shfl_sync(0xffffffffu, ahead.len, 0);
+            __syncwarp();
         }
         PtRecord rec{};
         bool ok = true;
@@ -482,9 +463,10 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
             return s;
         };
         const int page_boxes = a.page_size / PT_BOX;
+        const auto page_of = [&](int box) { return a.page_shift >= 0 ? box >> a.page_shift : box / page_boxes; };
         while (ok && x < end) {
             const int cost = cost_of(now), boxes = boxes_of(now), each = box_cost(now);
-            const long long all = pt_segments(a, now.rows) * cost;
+            const long long all = (long long)pt_segments(a, now.rows) * cost;
             if (x >= at + all) {
                 at += all;
                 seq++;
@@ -506,7 +488,9 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
                 to = cost;
             }
             // a box is the share's in which its cost begins
-            const int b0 = min((from + each - 1) / each, boxes), b1 = min((to + each - 1) / each, boxes);
+            constexpr uint32_t INV2 = (uint32_t)(((1ull << 32) + PT_C2 - 1) / PT_C2), INV4 = (uint32_t)(((1ull << 32) + PT_C4 - 1) / PT_C4);
+            const uint32_t inverse = each == 2 ? 0x80000000u : each == PT_C2 ? INV2 : INV4;  // (exact below 2^30)
+            const int b0 = min((int)__umulhi(from + each - 1, inverse), boxes), b1 = min((int)__umulhi(to + each - 1, inverse), boxes);
             if (b0 >= b1 && !(boxes == 0 && from == 0)) continue;
             const int qblk = (int)pt_div(seg, a.Hk), head = (int)(seg - (long long)qblk * a.Hk);
             int part = 0;
@@ -537,7 +521,7 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
                 const int chunk = (b - b0) & 31;
                 if (chunk == 0) {  // the pages of the next 32 boxes
                     const int mine_b = b + lane;
-                    page = mine_b < b1 ? __ldcg(a.block_table + seq * a.table_stride + mine_b / page_boxes) : -1;
+                    page = mine_b < b1 ? __ldcg(a.block_table + seq * a.table_stride + page_of(mine_b)) : -1;
                     if (page >= a.n_pages) page = -1;
                 }
                 const int n_box = min(4, b1 - b), j = lane >> 1;
@@ -561,7 +545,7 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
                 }
                 __syncwarp();
                 if (copy) {
-                    const int box = b + j, y = (box % page_boxes) * PT_BOX;
+                    const int box = b + j, y = (box - page_of(box) * page_boxes) * PT_BOX;
                     const uint32_t dst = smem_u32(ring + st * F::STAGE + (lane & 1) * (PT_STAGE * RB) + j * (PT_BOX * RB));
                     tma_load_5d(dst, (lane & 1) ? &mv : &mk, &full[st], y, head, my_page);
                 }
