@@ -93,7 +93,7 @@ Scratch scratch_of(const sparsk_paged_attn_args *a)
 }
 
 template <int HD, int CT, bool P2>
-cudaError_t launch(const PtArgs &p, const CUtensorMap &mk, const CUtensorMap &mv, int shares, bool join, cudaStream_t st)
+cudaError_t launch(const PtArgs &p, const CUtensorMap &mk, const CUtensorMap &mv, int shares, int join, cudaStream_t st)
 {
     static PerDevice<bool> ready;
     constexpr int smem = PtForm<HD, CT>::SMEM;
@@ -114,10 +114,11 @@ cudaError_t launch(const PtArgs &p, const CUtensorMap &mk, const CUtensorMap &mv
     cfg.numAttrs = 1;
     cudaError_t e = cudaLaunchKernelEx(&cfg, paged_attn_kernel<HD, CT, P2>, p, mk, mv);
     if (e != cudaSuccess || !join) return e;
-    cfg.gridDim = dim3(shares, 4 * p.tiles);
+    cfg.gridDim = dim3(shares, join * p.tiles);
     cfg.blockDim = dim3(PJ_THREADS);
     cfg.dynamicSmemBytes = 0;
-    return cudaLaunchKernelEx(&cfg, paged_join_kernel<HD, PtForm<HD, CT>::ES>, p, shares);
+    constexpr int ES = PtForm<HD, CT>::ES;
+    return join == 1 ? cudaLaunchKernelEx(&cfg, paged_join_kernel<HD, ES, 1>, p, shares) : cudaLaunchKernelEx(&cfg, paged_join_kernel<HD, ES, 4>, p, shares);
 }
 // A softmax weight is rounded to 16 bits where it meets the values; where that is no finer than the output's own
 // rounding, a second term carries the rest.
@@ -172,16 +173,16 @@ extern "C" int sparsk_paged_attention(const sparsk_paged_attn_args *a, void *scr
     p.q_wide = wide(a->q, 2, a->q_row_stride, a->q_head_stride);
     p.out_words = aligned(a->out, 4) && a->out_row_stride % 2 == 0 && a->out_head_stride % 2 == 0;
     int shares = std::min(PT_CTAS * n_sm, PT_MAX_SHARES);
-    bool join = true;
+    const int64_t segs = ((int64_t)a->n_rows * p.G / (16 * p.tiles) + a->n_seqs) * p.Hk;  // no more than so many
+    int join = segs * 8 <= shares ? 4 : 1;  // parts of a tile that the join deals out (0: no join)
     if (a->max_len > 0) {
         // no more CTAs than there can be shares, and no join where no segment is long enough to be cut (if one is all
         // the same, its share takes the whole of it)
         const int64_t boxes = ((int64_t)a->max_len + PT_BOX - 1) / PT_BOX;
-        const int64_t segs = ((int64_t)a->n_rows * p.G / (16 * p.tiles) + a->n_seqs) * p.Hk;
         shares = (int)std::max<int64_t>(1, std::min<int64_t>(shares, segs * (boxes * PT_C4 + PT_END_COST) / PT_MIN_SHARE + 1));
         if (boxes <= PT_WHOLE) {
             p.whole_boxes = INT_MAX;
-            join = false;
+            join = 0;
         }
     }
     const cudaError_t e = a->pool.head_dim == 64 ? launch_types<64>(a->pool.type, a->q_type, p, mk, mv, shares, join, (cudaStream_t)cuda_stream)

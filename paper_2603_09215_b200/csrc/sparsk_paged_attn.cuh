@@ -124,6 +124,11 @@ __device__ __forceinline__ uint32_t pt_widen(uint32_t two)
     asm("{\n\t.reg .b16 x;\n\tcvt.u16.u32 x, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, x;\n\t}" : "=r"(r) : "r"(two));
     return r;
 }
+// four of them at once
+__device__ __forceinline__ void pt_widen4(uint32_t four, uint32_t &lo, uint32_t &hi)
+{
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(four));
+}
 // Two query numbers in the type that meets the pool's: a number beyond fp16 as its largest.
 template <int CT>
 __device__ __forceinline__ uint32_t pt_query2(uint32_t w, int q_type)
@@ -205,9 +210,7 @@ __device__ __forceinline__ void pt_values(float (&o)[HD / 8][4], const uint32_t 
         for (int i = 0; i < 4; i++) {
             if constexpr (F::ES == 1) {
                 // a word holds two positions of two dimensions: dimension by dimension
-                const uint32_t x = __byte_perm(vb[i], 0, 0x3120);
-                w[(i >> 1) * 4 + (i & 1)] = pt_widen(x);
-                w[(i >> 1) * 4 + 2 + (i & 1)] = pt_widen(x >> 16);
+                pt_widen4(__byte_perm(vb[i], 0, 0x3120), w[(i >> 1) * 4 + (i & 1)], w[(i >> 1) * 4 + 2 + (i & 1)]);
             } else w[i] = vb[i];
         }
         if (ODD) {
@@ -406,6 +409,7 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
                 if (seg.y < 0) break;
                 const int v_first = seg.z * a.tiles * 16, n_here = min(seg.y * a.G - v_first, a.tiles * 16);
                 unsigned char *dst = queries + slot * a.tiles * F::QTILE;
+#pragma unroll 4
                 for (int i = tid - (PT_WARPS + 1) * 32; i < n_here * (HD / 8); i += PT_Q_WARPS * 32) {
                     const int v = i / (HD / 8), c = i % (HD / 8), r = pt_row_of(a, v_first + v);
                     const uint16_t *src = reinterpret_cast<const uint16_t *>(a.q) + (seg.x + r) * a.q_row_stride +
@@ -661,10 +665,13 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
                     pt_mma<CT>(s[1][1], qa[ks + 1], kb2[2], kb2[3]);
                 } else {
                     ldsm_x4(kb, K + F::turn(k_at, ks));
-                    pt_mma<CT>(s[0][0], qa[ks], pt_widen(kb[0]), pt_widen(kb[0] >> 16));
-                    pt_mma<CT>(s[0][1], qa[ks], pt_widen(kb[2]), pt_widen(kb[2] >> 16));
-                    pt_mma<CT>(s[1][0], qa[ks + 1], pt_widen(kb[1]), pt_widen(kb[1] >> 16));
-                    pt_mma<CT>(s[1][1], qa[ks + 1], pt_widen(kb[3]), pt_widen(kb[3] >> 16));
+                    uint32_t w[8];
+#pragma unroll
+                    for (int i = 0; i < 4; i++) pt_widen4(kb[i], w[2 * i], w[2 * i + 1]);
+                    pt_mma<CT>(s[0][0], qa[ks], w[0], w[1]);
+                    pt_mma<CT>(s[0][1], qa[ks], w[4], w[5]);
+                    pt_mma<CT>(s[1][0], qa[ks + 1], w[2], w[3]);
+                    pt_mma<CT>(s[1][1], qa[ks + 1], w[6], w[7]);
                 }
             }
             // a box that every vector sees whole needs no mask
@@ -842,64 +849,83 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
 
 // ------------------------------------------------------------------ the join
 // Share `blockIdx.x` ends in the middle of a segment: its last partial and the first ones of the shares behind it, up to
-// the one in which the segment ends.  blockIdx.y: which block of 16 vectors, and which quarter of the accumulators.
-template <int HD, int ES>
+// the one in which the segment ends.  blockIdx.y: which tile of 16 vectors, and which of PARTS parts of its accumulators: one where
+// segments are many and a segment's partials two or three (blocks that start and end are then what the join costs), four
+// where a few segments lie in tens of shares each.
+template <int HD, int ES, int PARTS>
 static __global__ void __launch_bounds__(PJ_THREADS) paged_join_kernel(const PtArgs a, int shares)
 {
-    // a block takes a quarter of a tile's accumulators: QP pairs of products, GROUPS partials side by side
-    constexpr int NT = HD / 8, QP = NT / 8, COLS = QP * 32, GROUPS = PJ_THREADS / COLS, PER = PJ_THREADS / 16;
+    // a block takes a tile's accumulators or a quarter of them: QP pairs of products, GROUPS partials side by side
+    constexpr int NT = HD / 8, QP = NT / 2 / PARTS, COLS = QP * 32, GROUPS = PJ_THREADS / COLS, PER = PJ_THREADS / 16;
     constexpr float LN2 = 0.6931471805599453f;
+    constexpr int FIRST = 4;  // partials a thread asks for before it knows their weights
     __shared__ float weight[PT_MAX_SHARES][16], red[PER][16], sums[PER][16];
-    __shared__ float4 acc[GROUPS][COLS][2];
-    const int w0 = blockIdx.x, mt = blockIdx.y >> 2, quarter = blockIdx.y & 3, tid = threadIdx.x, lane = tid & 31;
+    __shared__ float4 acc[GROUPS > 1 ? GROUPS : 1][COLS][2];
+    const int w0 = blockIdx.x, mt = blockIdx.y / PARTS, quarter = blockIdx.y % PARTS, tid = threadIdx.x, lane = tid & 31;
     griddep_wait();
     // the record, and where the segment ends: every warp for itself
     const int4 rec = __ldcg(reinterpret_cast<const int4 *>(&a.records[w0]));
     const int head = __ldcg(&a.records[w0].head);
-    int ends = w0 + 1 + lane < shares ? __ldcg(&a.records[w0 + 1 + lane].flags) & 4 : 0;
+    int ends[2];
+#pragma unroll
+    for (int k = 0; k < 2; k++) ends[k] = w0 + 1 + k * 32 + lane < shares ? __ldcg(&a.records[w0 + 1 + k * 32 + lane].flags) & 4 : 0;
     if (!(rec.x & 1)) return;
     const int row0 = rec.y, v0 = (rec.w * a.tiles + mt) * 16, n_vec = rec.z * a.G;
     if (v0 >= n_vec) return;
     int n = 1;
     for (int w = w0 + 1;;) {
-        const uint32_t b = __ballot_sync(0xffffffffu, ends);
-        n += b ? __ffs(b) : min(32, shares - w);
-        w += 32;
-        if (b || w >= shares) break;
-        ends = w + lane < shares ? __ldcg(&a.records[w + lane].flags) & 4 : 0;
+        const uint32_t b0 = __ballot_sync(0xffffffffu, ends[0]), b1 = __ballot_sync(0xffffffffu, ends[1]);
+        n += b0 ? __ffs(b0) : b1 ? 32 + __ffs(b1) : min(64, shares - w);
+        w += 64;
+        if (b0 || b1 || w >= shares) break;
+#pragma unroll
+        for (int k = 0; k < 2; k++) ends[k] = w + k * 32 + lane < shares ? __ldcg(&a.records[w + k * 32 + lane].flags) & 4 : 0;
     }
     const auto cell = [&](int i) { return ((size_t)(w0 + i) * 2 + (i == 0 ? 1 : 0)) * a.tiles + mt; };
+    const int col = tid % COLS, grp = tid / COLS, nt = (quarter * QP + col / 32) * 2;
+    const auto partial = [&](int i, float4 (&y)[2]) {
+#pragma unroll
+        for (int k = 0; k < 2; k++) y[k] = __ldcg(&a.part_o[(cell(i) * NT + nt + k) * 32 + lane]);
+    };
+    float4 early[FIRST][2];
+#pragma unroll
+    for (int k = 0; k < FIRST; k++)
+        if (grp + k * GROUPS < n) partial(grp + k * GROUPS, early[k]);
     // weights of the partials for each vector
     const int v = tid & 15, i0 = tid >> 4;
-    float top = -INFINITY;
+    float top = -INFINITY, sum = 0.f;  // (of a thread's own partials, the sum relative to their largest)
     for (int i = i0; i < n; i += PER) {
-        const float m = __ldcg(&a.part_ml[cell(i) * 16 + v]).x;
-        weight[i][v] = m;
-        top = fmaxf(top, m);
+        const float2 ml = __ldcg(&a.part_ml[cell(i) * 16 + v]);
+        weight[i][v] = ml.x;
+        const float m = fmaxf(top, ml.x), use = m == -INFINITY ? 0.f : m;
+        sum = sum * exp2f(top - use) + ml.y * exp2f(ml.x - use);
+        top = m;
     }
+    const float mine = top;
     red[i0][v] = top;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < PER; i++) top = fmaxf(top, red[i][v]);
     const float use = top == -INFINITY ? 0.f : top;
-    float sum = 0.f;
-    for (int i = i0; i < n; i += PER) {
-        const float f = exp2f(weight[i][v] - use);
-        weight[i][v] = f;
-        sum += f * __ldcg(&a.part_ml[cell(i) * 16 + v]).y;
-    }
-    sums[i0][v] = sum;
+    for (int i = i0; i < n; i += PER) weight[i][v] = exp2f(weight[i][v] - use);
+    sums[i0][v] = sum * exp2f(mine - use);
     __syncthreads();
-    const int col = tid % COLS, grp = tid / COLS, nt = (quarter * QP + col / 32) * 2;
     float4 x[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-#pragma unroll 8
-    for (int i = grp; i < n; i += GROUPS) {
+    const auto add = [&](int i, const float4 (&y)[2]) {
         const float f0 = weight[i][lane >> 2], f1 = weight[i][(lane >> 2) + 8];
 #pragma unroll
         for (int k = 0; k < 2; k++) {
-            const float4 y = __ldcg(&a.part_o[(cell(i) * NT + nt + k) * 32 + lane]);
-            x[k].x += f0 * y.x; x[k].y += f0 * y.y; x[k].z += f1 * y.z; x[k].w += f1 * y.w;
+            x[k].x += f0 * y[k].x; x[k].y += f0 * y[k].y; x[k].z += f1 * y[k].z; x[k].w += f1 * y[k].w;
         }
+    };
+#pragma unroll
+    for (int k = 0; k < FIRST; k++)
+        if (grp + k * GROUPS < n) add(grp + k * GROUPS, early[k]);
+#pragma unroll 4
+    for (int i = grp + FIRST * GROUPS; i < n; i += GROUPS) {
+        float4 y[2];
+        partial(i, y);
+        add(i, y);
     }
     acc[grp][col][0] = x[0];
     acc[grp][col][1] = x[1];
