@@ -320,9 +320,9 @@ def _page_pool(k: torch.Tensor, v: torch.Tensor, k_scale, v_scale):
     """(fields of PagePool, device, kv heads, head_dim).  Pools as [n_pages, n_kv_heads, page_size, head_dim]; pools whose positions lie before their heads come
     transposed (`x.transpose(1, 2)`)."""
     dev, shape, st = k.get_device(), k.shape, k.stride()
-    _need(dev >= 0 and v.get_device() == dev, "the pools are on one CUDA device")
-    _need(len(shape) == 4 and v.shape == shape and v.stride() == st and v.dtype is k.dtype, "pools of one shape, layout and type")
-    _need(st[3] == 1, "a head's numbers are contiguous")
+    if not (dev >= 0 and len(shape) == 4 and st[3] == 1 and v.shape == shape and v.stride() == st and v.dtype is k.dtype
+            and v.get_device() == dev):
+        raise SparskError(EINVAL, "pools: two of one shape, layout and type on one CUDA device, a head's numbers contiguous")
     ks = 0 if k_scale is None else _vec(k_scale, torch.float32, shape[1], dev, "k_scale")
     vs = 0 if v_scale is None else _vec(v_scale, torch.float32, shape[1], dev, "v_scale")
     return ((k.data_ptr(), v.data_ptr(), ks, vs, st[0], st[1], st[2], _TYPES.get(k.dtype, -1), *shape), dev, shape[1], shape[3])
@@ -337,10 +337,10 @@ def _rows(t: torch.Tensor, n: int, heads: int, head_dim: int, dev: int, what: st
 
 
 def _table(t: torch.Tensor, n: int, dev: int):
-    st = t.stride()
-    _need(t.dtype is torch.int32 and t.dim() == 2 and t.shape[0] >= n and st[1] == 1 and t.get_device() == dev,
-          "block_table: int32 [sequences, blocks], a row's entries contiguous")
-    return t.data_ptr(), st[0], t.shape[1]
+    st, shape = t.stride(), t.shape
+    if not (t.dtype is torch.int32 and len(shape) == 2 and shape[0] >= n and st[1] == 1 and t.get_device() == dev):
+        raise SparskError(EINVAL, "block_table: int32 [sequences, blocks], a row's entries contiguous")
+    return t.data_ptr(), st[0], shape[1]
 
 
 def page_map(lens: torch.Tensor, rows: torch.Tensor, block_table: torch.Tensor, ring: torch.Tensor, old_queue: torch.Tensor,
@@ -429,8 +429,11 @@ def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     if scratch is None:
         nbytes = load().sparsk_paged_attention_scratch_bytes(a)
         _need(nbytes > 0, "sparsk_paged_attention: a size, type, stride or address that it does not take")
-        scratch = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
-    _launch("sparsk_paged_attention", dev, a, _vec(scratch, torch.uint8, 1, dev, "scratch"), scratch.numel())
+        scratch = torch.empty(nbytes, dtype=torch.uint8, device=q.device)  # (held until the launch; then the stream's order keeps it)
+        at = scratch.data_ptr()
+    else:
+        at, nbytes = _vec(scratch, torch.uint8, 1, dev, "scratch"), scratch.numel()
+    _launch("sparsk_paged_attention", dev, a, at, nbytes)
     return out
 
 
