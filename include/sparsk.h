@@ -417,8 +417,8 @@ int sparsk_paged_attention(const sparsk_paged_attn_args *args /*host*/, void *sc
  * w = exp((z - max z) / temperature): the first top_k ids stay (0 or less: all); of those the shortest prefix whose mass
  * reaches top_p times theirs (1 or more: all); of those the ids with w >= min_p (0 or less: all); at least
  * one.  The token is the first id at which the cumulative mass exceeds uniforms[r] (in [0, 1)) times the
- * kept mass.  A temperature of 0 (or less, or NaN) takes the first id of the order.  logprob[r] (may be
- * NULL) is the logarithm of the token's softmax(z / temperature) over all of the row's ids (temperature 1 where it is 0 or less).
+ * kept mass.  A temperature of 0 (below 2^-126, or NaN) takes the first id of the order.  logprob[r] (may be
+ * NULL) is the logarithm of the token's softmax(z / temperature) over all of the row's ids (temperature 1 where the first id is taken).
  * A row without ids gets -1 and minus infinity.  Settings are DEVICE arrays [n_rows]; NULL stands for temperature 1, no
  * cut, all ids.  The masses are exact to about 2^-40 of the whole and do not depend on the order in which the GPU adds them: the same
  * call draws the same token.  Logits are only read; rows lie row_stride elements apart.  Enqueued on `cuda_stream`;

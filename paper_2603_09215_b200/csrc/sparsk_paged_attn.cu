@@ -66,7 +66,7 @@ bool paged_attn_ok(const sparsk_paged_attn_args *a)
     if (a->max_rows < 0 || a->max_len < 0 || (!a->row_start && a->n_rows != a->n_seqs)) return false;
     if (!(a->scale >= 0.f) || !(a->scale < INFINITY)) return false;
     if (a->table_stride < a->max_blocks || a->table_stride > INT_MAX) return false;
-    if ((int64_t)a->max_blocks * a->pool.page_size > INT_MAX || (int64_t)a->n_rows * a->n_q_heads > INT_MAX / 2) return false;
+    if ((int64_t)a->max_blocks * a->pool.page_size > INT_MAX - 64 || (int64_t)a->n_rows * a->n_q_heads > INT_MAX / 2) return false;
     return strides_ok(a->q_row_stride, a->q_head_stride) && strides_ok(a->out_row_stride, a->out_head_stride);
 }
 

@@ -115,7 +115,7 @@ static __global__ void __launch_bounds__(T, 512 / T) settings_sample_kernel(spar
     uint32_t *slice = reinterpret_cast<uint32_t *>(own_count + OWN);
     __shared__ StShared sh;
     const int row = blockIdx.x / C, rank = Cl::rank(), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int lo = a.id_lo ? max(a.id_lo[row], 0) : 0, hi = a.id_hi ? min(a.id_hi[row], a.n_ids) : a.n_ids;
+    const int lo = a.id_lo ? min(max(a.id_lo[row], 0), a.n_ids) : 0, hi = a.id_hi ? min(max(a.id_hi[row], 0), a.n_ids) : a.n_ids;
     const int n = max(hi - lo, 0), per_cta = (n + C - 1) / C, beg = min(rank * per_cta, n), mine = min(per_cta, n - beg),
               mine4 = (mine + 3) & ~3;  // (filled up with ids that nobody draws)
 

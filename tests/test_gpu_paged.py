@@ -370,6 +370,25 @@ def test_attention_bad_row_starts_stay_inside(B):
     assert bool((out[:3] == 5.0).all()) and bool((out[6:] == 5.0).all())
 
 
+@pytest.mark.parametrize("max_rows,max_len", [(1, 1), (1, 128), (2, 300), (64, 100000), (0, 0), (8, 129)])
+def test_attention_hints_change_no_result(B, max_rows, max_len):
+    """What the caller knows of rows and lengths, understated (segments are then not cut, or tiles come in several blocks) or
+    overstated."""
+    lens, rows = [300, 5, 2000, 128, 129], [3, 1, 9, 2, 1]
+    q, kc, vc, table, start, sc = attn_case(lens, rows, 14, 2, 64, 16, BF, FP, "hnd", 21)
+    check_attn(B, q, kc, vc, table, lens, start, sc, max_rows=max_rows, max_len=max_len)
+
+
+def test_attention_many_sequences(B):
+    """More sequences than a CTA has threads, most of them short, some without rows."""
+    rng = np.random.default_rng(0)
+    lens = [int(x) for x in rng.integers(0, 40, 700)]
+    rows = [int(x) for x in rng.integers(0, 3, 700)]
+    lens[13], lens[600], rows[13], rows[600] = 900, 1500, 1, 2
+    q, kc, vc, table, start, sc = attn_case(lens, rows, 4, 2, 64, 16, BF, FP, "nhd", 22)
+    check_attn(B, q, kc, vc, table, lens, start, sc, max_rows=2, max_len=1500)
+
+
 def test_attention_strides(B):
     """Queries and outputs as slices of wider rows, heads apart, any element as the first."""
     lens = [33, 100]
@@ -490,6 +509,10 @@ def test_sample_settings_out_of_range(B):
                                 min_p=f([nan, -1.0, 0.0, -inf] * 2)), want)
     first = B.sample(z, f([0.0] * 8))
     assert torch.equal(B.sample(z, f([nan, -1.0, -inf, 0.0] * 2)), first)
+    # id ranges: cut to the row, empty where they run backwards
+    lo, hi = ints([-2 ** 31, 5, 300, 2 ** 31 - 1, 0, 7, 0, 299]), ints([2 ** 31 - 1, -2 ** 31, 301, 2 ** 31 - 1, 0, 3, 300, 2 ** 31 - 1])
+    got = B.sample(z, u, id_lo=lo, id_hi=hi)
+    assert got[[0, 6]].tolist() == want[[0, 6]].tolist() and got[1:6].tolist() == [-1] * 5 and int(got[7]) == 299
     flat = torch.zeros((2, 300), device="cuda")
     assert B.sample(flat, f([1.0, 5.0])).tolist() == [299, 299]
     assert B.sample(flat, f([0.5, 0.5]), temperature=f([inf, inf])).tolist() == [150, 150]
