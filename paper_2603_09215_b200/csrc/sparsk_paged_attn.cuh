@@ -36,7 +36,7 @@ constexpr int PT_MAX_SHARES = 2 * 160;         // CTAs of a launch (the scratch 
 constexpr int PT_END_COST = 24;                // a segment's set-up and end, in the unit of PtForm::box_cost
 constexpr int PT_WHOLE = 8;                    // a segment of up to so many boxes is never cut
 constexpr int PT_MIN_SHARE = 28;               // the same unit
-constexpr int PT_C2 = 3, PT_C4 = 6;
+constexpr int PT_C2 = 3, PT_C4 = 5;
 constexpr float PT_LAG = 8.f;                  // in powers of two
 constexpr int PT_RING_BYTES = 112 * 1024;      // of a CTA's shared memory: boxes, queries, sums that meet
 constexpr int PJ_THREADS = 256;
