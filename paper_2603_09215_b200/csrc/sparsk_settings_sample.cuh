@@ -208,8 +208,10 @@ static __global__ void __launch_bounds__(T, 512 / T) settings_sample_kernel(spar
 
     // ---- the bins
     // Adds the ids for which `which` names a bin into them: h in one word, ids (upper half) and carries of h (lower half) in the
-    // other.  Warps whose ids all fall into one bin add up first.
-    const auto fill = [&](auto which) {
+    // other.  Warps whose ids all fall into one bin add up first; what lies beyond a whole row's range (ids that a program has ruled
+    // out by the type's lowest value, say) is only counted, by every thread for itself.
+    const auto fill = [&](auto which, bool whole_row) {
+        int beyond = 0;
         const auto at = [&](int i) { return i < mine4 ? *reinterpret_cast<const uint4 *>(slice + i) : make_uint4(ST_DEAD, ST_DEAD, ST_DEAD, ST_DEAD); };
         uint4 after = at(tid * 4);
         for (int i0 = warp * 128; i0 < mine4; i0 += T * 4) {
@@ -222,7 +224,11 @@ static __global__ void __launch_bounds__(T, 512 / T) settings_sample_kernel(spar
             for (int k = 0; k < 4; k++) {
                 const double y = place(word[k]);
                 b[k] = word[k] == ST_DEAD ? -1 : which(word[k], y);
-                h[k] = bin_of(y) == ST_BINS - 1 ? 0u : h_of(y);
+                h[k] = h_of(y);
+                if (whole_row && b[k] == ST_BINS - 1) {
+                    beyond++;
+                    b[k] = -1;
+                }
             }
             const int b0 = __shfl_sync(0xffffffffu, b[0], 0);
             if (b0 >= 0 && __all_sync(0xffffffffu, b[0] == b0 && b[1] == b0 && b[2] == b0 && b[3] == b0)) {
@@ -249,6 +255,8 @@ static __global__ void __launch_bounds__(T, 512 / T) settings_sample_kernel(spar
                     if (b[k] >= 0) atomicAdd(bin_hi + b[k], 0x10000u + (old[k] + h[k] < old[k] ? 1u : 0u));
             }
         }
+        beyond = __reduce_add_sync(0xffffffffu, beyond);
+        if (lane == 0 && beyond) atomicAdd(bin_hi + ST_BINS - 1, (uint32_t)beyond << 16);
     };
     // The largest key below the top for which `holds`, which no larger one may follow; 0 if none does.  Five bits at a time.
     const auto last_key = [&](auto holds) {
@@ -454,7 +462,7 @@ static __global__ void __launch_bounds__(T, 512 / T) settings_sample_kernel(spar
         }
         __syncthreads();
     };
-    fill([&](uint32_t, double y) { return bin_of(y); });
+    fill([&](uint32_t, double y) { return bin_of(y); }, true);
     add_up([&](int b) { return exp(-(double)b / s); }, PER > 1 ? exp(-1.0 / s) : 1.0, true);
     const unsigned long long total = sh.all_mass[C];
     const auto logprob = [&](uint32_t key) { return (float)(log_weight(key) - log((double)total / ST_UNIT)); };
@@ -516,7 +524,7 @@ static __global__ void __launch_bounds__(T, 512 / T) settings_sample_kernel(spar
         }
         if (divided) {  // back to the bins of the whole row
             clear_bins();
-            fill([&](uint32_t, double y) { return bin_of(y); });
+            fill([&](uint32_t, double y) { return bin_of(y); }, true);
             add_up([&](int b) { return exp(-(double)b / s); }, PER > 1 ? exp(-1.0 / s) : 1.0, true);
             divided = false;
             gathered = -1;
@@ -555,7 +563,7 @@ static __global__ void __launch_bounds__(T, 512 / T) settings_sample_kernel(spar
                 const int shift = max(0, 32 - __clz(k_hi - k_lo) - 11);  // 2,048 bins cover k_hi - k_lo < 2^(shift + 11)
                 clear_bins();
                 const double e_bin = bin == ST_BINS - 1 ? 0.0 : exp(-(double)bin / s);
-                fill([&](uint32_t bits, double) { return st_key(bits) - k_lo <= k_hi - k_lo ? (int)((k_hi - st_key(bits)) >> shift) : -1; });
+                fill([&](uint32_t bits, double) { return st_key(bits) - k_lo <= k_hi - k_lo ? (int)((k_hi - st_key(bits)) >> shift) : -1; }, false);
                 add_up([&](int) { return e_bin; }, 1.0, false);
                 const int b_all = before;
                 const unsigned long long m_all = mass_before;
