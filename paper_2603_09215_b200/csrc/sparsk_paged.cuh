@@ -15,7 +15,8 @@ namespace sparsk {
 // the queue and not from the table), so every block works the sums out for itself
 // and the blocks share the rows and pages without waiting for one another: one launch.
 // Latency is all there is to it (a step of 64 sequences writes about a kilobyte): two trips to the memory and the
-// sums between them, so no 64-bit division, and a row a thread.
+// sums between them, so no 64-bit division, and a row a thread.  64 sequences of one row: 3.6 us (6.4 with 64-bit sums and
+// divisions), 300 sequences with 24 prompts, 33,000 rows: 6 us (11.8 with four rows a thread).
 constexpr int PM_THREADS = 1024;
 constexpr uint32_t PM_MOST = 0x7fffffffu;  // sums end here: whatever the lengths say, none of them wraps
 

@@ -16,8 +16,14 @@
 // vectors, two boxes each for one of two tiles of 16 where it has up to 32, else all four for one of four.  Every warp
 // keeps the softmax of its own positions; the warps of one tile meet at the segment's end only.  8-bit pages are widened to fp16 in
 // registers, between the shared memory and the product.
-// Bound by HBM: a position of a head of 128 fp16 numbers is 512 bytes, 23 of which come per clock and SM, so 16 positions
-// may take 350 clocks of an SM.
+// Bound by HBM where a segment has one tile of query vectors: a position of a head of 128 fp16 numbers is 512 bytes, 23 of which
+// come per clock and SM, so 16 positions may take 350 clocks of an SM; eight computing warps need about 240.  64 sequences of
+// 8,192 positions (32 heads on 2, bf16): 537 MB in 92 us, 5.8 TB/s of 6.5 that a copy reaches; 64 of 256 to 2,048 (28 on 4, fp16): 152 MB
+// in 35.2 us, of which the first copies take 3, the segments' ends and the join 5.  With three or four tiles the warps' instructions
+// bound it (about 330 a box and tile, widening of 8-bit pages among them): 48 refresh blocks of up to four rows, 32 heads on 2:
+// 60 MB of e4m3 in 47 us, 120 MB of fp16 in 41.  Two boxes side by side in a warp gave those 45 and 42, and cost single rows 4 %.
+// What a share waits for at its start is instructions that no warp of the SM has met yet, more than memory: divisions
+// out of line, one code for all tile counts.
 #pragma once
 
 #include <cuda_fp8.h>
@@ -28,15 +34,14 @@
 namespace sparsk {
 
 constexpr int PT_THREADS = 256, PT_WARPS = 4, PT_Q_WARPS = 3;  // four warps compute, one brings the boxes, three the queries
-// registers are given out by fours of warps, and the four that compute take most of what the others were launched with
-constexpr int PT_REGS = 200, PT_REGS_BRING = 56; // (times 128 threads each: the launch's 128 times 256)
+// Registers are given out by fours of warps, and the four that compute take most of what the others were launched with.
+constexpr int PT_REGS = 200, PT_REGS_BRING = 56;  // (times 128 threads each: the launch's 128 times 256)
 constexpr int PT_BOX = 16, PT_STAGE = 64;      // positions
 constexpr int PT_CTAS = 2;                     // resident on an SM
 constexpr int PT_MAX_SHARES = 2 * 160;         // CTAs of a launch (the scratch is sized for them)
-constexpr int PT_END_COST = 24;                // a segment's set-up and end, in the unit of PtForm::box_cost
+constexpr int PT_END_COST = 24;                // a segment's set-up and end, in the unit of PtForm::box_cost (16 or 36: 1 to 2 % more)
 constexpr int PT_WHOLE = 8;                    // a segment of up to so many boxes is never cut
-constexpr int PT_MIN_SHARE = 28;               // the same unit
-constexpr int PT_C2 = 3, PT_C4 = 5;
+constexpr int PT_MIN_SHARE = 28;               // the same unit (38 put two short segments into one share: 9.0 us for 6.3)
 constexpr float PT_LAG = 8.f;                  // in powers of two
 constexpr int PT_RING_BYTES = 112 * 1024;      // of a CTA's shared memory: boxes, queries, sums that meet
 constexpr int PJ_THREADS = 256;
@@ -84,7 +89,9 @@ struct PtForm {
     static constexpr int SMEM = NS * STAGE + MEET + 4 * QTILE + NS * (16 + (int)sizeof(PtStage)) + 160 + PT_WARPS * 16 * 8 + 16;
     static_assert(PT_CTAS * (SMEM + 1024) <= 228 * 1024, "two CTAs share an SM");
     // What a box costs where the segment has one tile of vectors (the stage's boxes go to four warps), two (two by two) or more
-    // (every box to every warp).
+    // (every box to every warp).  48 refresh blocks over e4m3 / fp16 pages, us: 2, 3, 5 47.2 / 41.3; 2, 3, 6 50.1 / 43.5; 2, 3, 8 56.6 / 49.9; 2,
+    // 2, 5 56.5 / 48.4; 2, 4, 6 48.9 / 43.7 (and 28 vectors in fp16 56.1 for 51.9).
+    static constexpr int PT_C2 = 3, PT_C4 = 5;
     __device__ __forceinline__ static int box_cost(int vectors) { return vectors <= 16 ? 2 : vectors <= 32 ? PT_C2 : PT_C4; }
     // byte offset of 16-byte chunk c of row r inside a box
     __device__ __forceinline__ static int at(int r, int c)
@@ -492,8 +499,8 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
                 to = cost;
             }
             // a box is the share's in which its cost begins
-            constexpr uint32_t INV2 = (uint32_t)(((1ull << 32) + PT_C2 - 1) / PT_C2), INV4 = (uint32_t)(((1ull << 32) + PT_C4 - 1) / PT_C4);
-            const uint32_t inverse = each == 2 ? 0x80000000u : each == PT_C2 ? INV2 : INV4;  // (exact below 2^30)
+            constexpr uint32_t INV2 = (uint32_t)(((1ull << 32) + F::PT_C2 - 1) / F::PT_C2), INV4 = (uint32_t)(((1ull << 32) + F::PT_C4 - 1) / F::PT_C4);
+            const uint32_t inverse = each == 2 ? 0x80000000u : each == F::PT_C2 ? INV2 : INV4;  // (exact below 2^30)
             const int b0 = min((int)__umulhi(from + each - 1, inverse), boxes), b1 = min((int)__umulhi(to + each - 1, inverse), boxes);
             if (b0 >= b1 && !(boxes == 0 && from == 0)) continue;
             const int qblk = (int)pt_div(seg, a.Hk), head = (int)(seg - (long long)qblk * a.Hk);
