@@ -41,7 +41,8 @@ constexpr int PT_CTAS = 2;                     // resident on an SM
 constexpr int PT_MAX_SHARES = 2 * 160;         // CTAs of a launch (the scratch is sized for them)
 constexpr int PT_END_COST = 24;                // a segment's set-up and end, in the unit of PtForm::box_cost (16 or 36: 1 to 2 % more)
 constexpr int PT_WHOLE = 8;                    // a segment of up to so many boxes is never cut
-constexpr int PT_MIN_SHARE = 28;               // the same unit (38 put two short segments into one share: 9.0 us for 6.3)
+constexpr int PT_MIN_SHARE = 20;               // the same unit (40 puts two short segments into one share: 7.1 us for 5.1; one of 1,500
+                                               // positions 11.2 us, with 40 13.1, with 80 16.5)
 constexpr float PT_LAG = 8.f;                  // in powers of two
 constexpr int PT_RING_BYTES = 112 * 1024;      // of a CTA's shared memory: boxes, queries, sums that meet
 constexpr int PJ_THREADS = 256;
