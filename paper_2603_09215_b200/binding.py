@@ -1,14 +1,13 @@
 """Thin ctypes binding of the C ABI in ``include/sparsk.h``.
 
 Argument marshalling only: every step of the decode path runs in the CUDA kernels of
-``libsparsk.so``.  PyTorch is used for device memory and streams.  Importing this module
+``libsparsk.so``; the paged calls' tensors are marshalled by ``_paged.so``.  PyTorch is used for device memory and streams.  Importing this module
 fails loudly if the compiled library is missing; there is no CPU fallback.
 """
 from __future__ import annotations
 
 import ctypes as C
 import os
-import struct
 from typing import NamedTuple
 
 import numpy as np
@@ -94,15 +93,6 @@ class SampleArgs(C.Structure):
                                           "token", "logprob")] + [
         ("row_stride", C.c_int64)] + [(n, C.c_int32) for n in ("type", "n_rows", "n_ids")]
 
-
-# The same blocks packed in one go: filling a ctypes structure field by field costs up to 2 us a call.
-_POOL = "4Q3q5i4x"
-_PACK_MAP = struct.Struct("12Qq5i4x")
-_PACK_APPEND = struct.Struct(_POOL + "7Q8q5i4x")
-_PACK_ATTN = struct.Struct(_POOL + "6Q5q7if")
-_PACK_SAMPLE = struct.Struct("10Qq3i4x")
-for _p, _c in ((_PACK_MAP, PageMapArgs), (_PACK_APPEND, PagedAppendArgs), (_PACK_ATTN, PagedAttnArgs), (_PACK_SAMPLE, SampleArgs)):
-    assert _p.size == C.sizeof(_c), (_p.format, _c)
 
 _lib = None
 
@@ -271,9 +261,6 @@ def attention_scratch_bytes(n_rows: int, n_q_heads: int, head_dim: int) -> int:
 
 
 # ------------------------------------------------------------------ a paged cache
-_TYPES = {torch.float32: FP32, torch.bfloat16: BF16, torch.float16: FP16, torch.float8_e4m3fn: E4M3}
-
-
 class PageMap(NamedTuple):
     """What page_map writes: lengths and queue after the step, and of every row its sequence, position and slot."""
     seq_len: torch.Tensor
@@ -285,62 +272,23 @@ class PageMap(NamedTuple):
     status: torch.Tensor
 
 
-def _need(ok: bool, what: str):
-    if not ok:
-        raise SparskError(EINVAL, what)
+_paged = None
 
 
-def _pack(block: struct.Struct, *fields) -> bytes:
-    try:
-        return block.pack(*fields)
-    except struct.error as e:
-        raise SparskError(EINVAL, f"a size or stride that does not fit its field: {e}") from None
-
-
-def _vec(t: torch.Tensor, dtype, n: int, dev: int, what: str) -> int:
-    """Address of a contiguous array of at least n numbers on device `dev`."""
-    if t.dtype is not dtype or t.get_device() != dev or t.numel() < n or not t.is_contiguous():
-        raise SparskError(EINVAL, f"{what}: a contiguous {dtype} array of at least {n} numbers on cuda:{dev} is wanted")
-    return t.data_ptr()
-
-
-def _launch(name: str, dev: int, *args):
-    """One entry point, on the current stream of device `dev` whichever device is current."""
-    f = getattr(_lib or load(), name)
-    if torch._C._cuda_getDevice() == dev:
-        rc = f(*args, torch._C._cuda_getCurrentRawStream(dev))
-    else:
-        with torch.cuda.device(dev):
-            rc = f(*args, torch._C._cuda_getCurrentRawStream(dev))
-    if rc != OK:
-        raise SparskError(rc, name)
-
-
-def _page_pool(k: torch.Tensor, v: torch.Tensor, k_scale, v_scale):
-    """(fields of PagePool, device, kv heads, head_dim).  Pools as [n_pages, n_kv_heads, page_size, head_dim]; pools whose positions lie before their heads come
-    transposed (`x.transpose(1, 2)`)."""
-    dev, shape, st = k.get_device(), k.shape, k.stride()
-    if not (dev >= 0 and len(shape) == 4 and st[3] == 1 and v.shape == shape and v.stride() == st and v.dtype is k.dtype
-            and v.get_device() == dev):
-        raise SparskError(EINVAL, "pools: two of one shape, layout and type on one CUDA device, a head's numbers contiguous")
-    ks = 0 if k_scale is None else _vec(k_scale, torch.float32, shape[1], dev, "k_scale")
-    vs = 0 if v_scale is None else _vec(v_scale, torch.float32, shape[1], dev, "v_scale")
-    return ((k.data_ptr(), v.data_ptr(), ks, vs, st[0], st[1], st[2], _TYPES.get(k.dtype, -1), *shape), dev, shape[1], shape[3])
-
-
-def _rows(t: torch.Tensor, n: int, heads: int, head_dim: int, dev: int, what: str):
-    """(address, row stride, head stride) of [n, heads, head_dim]."""
-    st = t.stride()
-    if t.shape != (n, heads, head_dim) or st[2] != 1 or t.get_device() != dev:
-        raise SparskError(EINVAL, f"{what}: [{n}, {heads}, {head_dim}] on cuda:{dev}, the last dimension contiguous, is wanted")
-    return t.data_ptr(), st[0], st[1]
-
-
-def _table(t: torch.Tensor, n: int, dev: int):
-    st, shape = t.stride(), t.shape
-    if not (t.dtype is torch.int32 and len(shape) == 2 and shape[0] >= n and st[1] == 1 and t.get_device() == dev):
-        raise SparskError(EINVAL, "block_table: int32 [sequences, blocks], a row's entries contiguous")
-    return t.data_ptr(), st[0], shape[1]
+def _native():
+    """The compiled marshalling of the paged calls (``csrc/sparsk_torch.cpp``): every tensor is checked there."""
+    global _paged
+    if _paged is None:
+        L = load()
+        try:
+            from . import _paged as m
+        except ImportError as e:
+            raise ImportError(f"{_HERE}/_paged.so is missing or does not load ({e}): build it with"
+                              " `python -m paper_2603_09215_b200.build`") from e
+        m.bind(SparskError, *(C.cast(getattr(L, n), C.c_void_p).value for n in (
+            "sparsk_page_map", "sparsk_paged_append", "sparsk_paged_attention_scratch_bytes", "sparsk_paged_attention", "sparsk_sample")))
+        _paged = m
+    return _paged
 
 
 def page_map(lens: torch.Tensor, rows: torch.Tensor, block_table: torch.Tensor, ring: torch.Tensor, old_queue: torch.Tensor,
@@ -350,25 +298,16 @@ def page_map(lens: torch.Tensor, rows: torch.Tensor, block_table: torch.Tensor, 
     ended, its pages go back), and each new row's sequence, position and slot.  block_table and ring are changed in place; results go
     to the keyword arrays (as many rows as row_seq has), or to new ones of `max_rows` rows.  The status stays on
     the device: 0, or PAGES_* codes, and then nothing has moved."""
-    dev, n = lens.get_device(), lens.shape[0]
-    _need(dev >= 0, "the lengths are on a CUDA device")
-    _need(row_seq is not None or max_rows is not None, "max_rows or row_seq says how many rows the step may have")
-    m = row_seq.shape[0] if row_seq is not None else int(max_rows)
-    new = lambda k, dtype=torch.int32: torch.empty(k, dtype=dtype, device=lens.device)  # noqa: E731
-    out = PageMap(seq_len if seq_len is not None else new(n), queue if queue is not None else new(2),
-                  row_start if row_start is not None else new(n + 1), row_seq if row_seq is not None else new(m),
-                  row_pos if row_pos is not None else new(m), slot_map if slot_map is not None else new(m, torch.int64),
-                  status if status is not None else new(1))
-    table, stride, blocks = _table(block_table, n, dev)
-    i32 = torch.int32
-    a = _pack(_PACK_MAP, _vec(lens, i32, n, dev, "lens"), _vec(rows, i32, n, dev, "rows"), table, _vec(ring, i32, 1, dev, "ring"),
-                       _vec(old_queue, i32, 2, dev, "old_queue"), _vec(out.seq_len, i32, n, dev, "seq_len"),
-                       _vec(out.queue, i32, 2, dev, "queue"), _vec(out.row_start, i32, n + 1, dev, "row_start"),
-                       _vec(out.row_seq, i32, m, dev, "row_seq"), _vec(out.row_pos, i32, m, dev, "row_pos"),
-                       _vec(out.slot_map, torch.int64, m, dev, "slot_map"), _vec(out.status, i32, 1, dev, "status"),
-                       stride, n, blocks, page_size, ring.shape[0], m)
-    _launch("sparsk_page_map", dev, a)
-    return out
+    if seq_len is None or queue is None or row_start is None or row_seq is None or row_pos is None or slot_map is None or status is None:
+        if row_seq is None and max_rows is None:
+            raise SparskError(EINVAL, "max_rows or row_seq says how many rows the step may have")
+        n, m = lens.shape[0], row_seq.shape[0] if row_seq is not None else int(max_rows)
+        new = lambda t, k, dtype=torch.int32: torch.empty(k, dtype=dtype, device=lens.device) if t is None else t  # noqa: E731
+        seq_len, queue, row_start, status = new(seq_len, n), new(queue, 2), new(row_start, n + 1), new(status, 1)
+        row_seq, row_pos, slot_map = new(row_seq, m), new(row_pos, m), new(slot_map, m, torch.int64)
+    (_paged or _native()).page_map(lens, rows, block_table, ring, old_queue, page_size, seq_len, queue, row_start, row_seq, row_pos,
+                                   slot_map, status)
+    return PageMap(seq_len, queue, row_start, row_seq, row_pos, slot_map, status)
 
 
 def paged_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, slot_map: torch.Tensor, *,
@@ -376,31 +315,11 @@ def paged_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cach
                  rope: torch.Tensor | None = None, k_scale=None, v_scale=None) -> torch.Tensor | None:
     """sparsk_paged_append: k, v [n, n_kv_heads, head_dim] into their slots (int64 [n], -1: left out); with
     `rope` [positions, head_dim / 2, 2] (cosine, sine; float32) keys and queries q [n, n_q_heads, head_dim] are turned to
-    their positions row_pos (int32 [n]).  Returns the turned queries (q_out, or new: q's type, bf16 for fp32)."""
-    pool, dev, hk, hd = _page_pool(k_cache, v_cache, k_scale, v_scale)
-    n = k.shape[0]
-    kp, krs, khs = _rows(k, n, hk, hd, dev, "k")
-    vp, vrs, vhs = _rows(v, n, hk, hd, dev, "v")
-    _need(v.dtype is k.dtype, "k and v are of one type")
-    qp = qo = rp = rt = qrs = qhs = qors = qohs = hq = length = 0
-    qot = BF16
-    if q is not None:
-        hq = q.shape[1]
-        qp, qrs, qhs = _rows(q, n, hq, hd, dev, "q")
-        _need(q.dtype is k.dtype, "q and k are of one type")
-        if q_out is None:
-            q_out = torch.empty((n, hq, hd), dtype=torch.bfloat16 if q.dtype is torch.float32 else q.dtype, device=q.device)
-        qo, qors, qohs = _rows(q_out, n, hq, hd, dev, "q_out")
-        qot = _TYPES.get(q_out.dtype, -1)
-    if rope is not None:
-        _need(row_pos is not None and rope.dim() == 3 and rope.shape[1:] == (hd // 2, 2),
-              "rope: [positions, head_dim / 2, 2], and row_pos with it")
-        length = rope.shape[0]
-        rt, rp = _vec(rope, torch.float32, 1, dev, "rope"), _vec(row_pos, torch.int32, n, dev, "row_pos")
-    a = _pack(_PACK_APPEND, *pool, kp, vp, qp, qo, _vec(slot_map, torch.int64, n, dev, "slot_map"), rp, rt, krs, khs, vrs, vhs, qrs, qhs,
-                          qors, qohs, _TYPES.get(k.dtype, -1), qot, n, hq, length)
-    if n:
-        _launch("sparsk_paged_append", dev, a)
+    their positions row_pos (int32 [n]).  The pools are [n_pages, n_kv_heads, page_size, head_dim]; pools whose positions lie before
+    their heads come transposed (`x.transpose(1, 2)`).  Returns the turned queries (q_out, or new: q's type, bf16 for fp32)."""
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=torch.bfloat16 if q.dtype is torch.float32 else q.dtype, device=q.device)
+    (_paged or _native()).paged_append(k, v, k_cache, v_cache, slot_map, q, q_out, row_pos, rope, k_scale, v_scale)
     return q_out
 
 
@@ -412,28 +331,10 @@ def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     included) positions lie in the pages of block_table (int32 [sequences, blocks]).  Sequence i has rows row_start[i]
     to row_start[i + 1] - 1; without row_start every sequence has one.  max_rows and max_len, where known, size the launch.  `lse`
     (float32 [n, n_q_heads]) receives the logarithms of the softmax sums."""
-    pool, dev, _, head_dim = _page_pool(k_cache, v_cache, k_scale, v_scale)
-    n_seqs, (n, hq, hd) = seq_len.shape[0], q.shape
     if out is None:
-        out = torch.empty((n, hq, hd), dtype=q.dtype, device=q.device)
-    _need(out.dtype is q.dtype and hd == head_dim, "q and out are of one type, with the pool's head_dim")
-    qp, qrs, qhs = _rows(q, n, hq, hd, dev, "q")
-    op, ors, ohs = _rows(out, n, hq, hd, dev, "out")
-    table, stride, blocks = _table(block_table, n_seqs, dev)
-    a = _pack(_PACK_ATTN, *pool, qp, op, 0 if lse is None else _vec(lse, torch.float32, n * hq, dev, "lse"), table,
-                        _vec(seq_len, torch.int32, n_seqs, dev, "seq_len"),
-                        0 if row_start is None else _vec(row_start, torch.int32, n_seqs + 1, dev, "row_start"),
-                        stride, qrs, qhs, ors, ohs, _TYPES.get(q.dtype, -1), n, n_seqs, blocks, hq, max_rows, max_len, scale)
-    if n == 0:
-        return out
-    if scratch is None:
-        nbytes = load().sparsk_paged_attention_scratch_bytes(a)
-        _need(nbytes > 0, "sparsk_paged_attention: a size, type, stride or address that it does not take")
-        scratch = torch.empty(nbytes, dtype=torch.uint8, device=q.device)  # (held until the launch; then the stream's order keeps it)
-        at = scratch.data_ptr()
-    else:
-        at, nbytes = _vec(scratch, torch.uint8, 1, dev, "scratch"), scratch.numel()
-    _launch("sparsk_paged_attention", dev, a, at, nbytes)
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    (_paged or _native()).paged_attention(q, k_cache, v_cache, block_table, seq_len, row_start, max_rows, max_len, scale, k_scale,
+                                          v_scale, out, lse, scratch)
     return out
 
 
@@ -442,17 +343,9 @@ def sample(logits: torch.Tensor, uniforms: torch.Tensor, *, temperature=None, to
     """sparsk_sample: one token (int32 [n]) for each row of logits [n, ids] (float32, bf16 or fp16), drawn with uniforms
     (float32 [n]) by the row's own settings: float32 temperature, top_p, min_p and int32 top_k, id_lo, id_hi, each [n] on the
     device, or None.  `logprob` (float32 [n]) receives the tokens' log probabilities before the cuts."""
-    dev, (n, ids) = logits.get_device(), logits.shape
-    _need(dev >= 0 and (ids == 1 or logits.stride(1) == 1), "logits: [rows, ids] on a CUDA device, a row contiguous")
     if token is None:
-        token = torch.empty(n, dtype=torch.int32, device=logits.device)
-    f = lambda t, what: 0 if t is None else _vec(t, torch.float32, n, dev, what)  # noqa: E731
-    i = lambda t, what: 0 if t is None else _vec(t, torch.int32, n, dev, what)  # noqa: E731
-    a = _pack(_PACK_SAMPLE, logits.data_ptr(), f(uniforms, "uniforms"), f(temperature, "temperature"), f(top_p, "top_p"), f(min_p, "min_p"),
-                          i(top_k, "top_k"), i(id_lo, "id_lo"), i(id_hi, "id_hi"), i(token, "token"), f(logprob, "logprob"),
-                          logits.stride(0), _TYPES.get(logits.dtype, -1), n, ids)
-    if n:
-        _launch("sparsk_sample", dev, a)
+        token = torch.empty(logits.shape[0], dtype=torch.int32, device=logits.device)
+    (_paged or _native()).sample(logits, uniforms, temperature, top_k, top_p, min_p, id_lo, id_hi, token, logprob)
     return token
 
 

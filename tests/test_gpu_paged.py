@@ -603,3 +603,59 @@ def test_calls_that_overlap(B):
                 got.append(B.paged_attention(q, kc, vc, t, n))
     torch.cuda.synchronize()
     assert all(torch.equal(g, want) for g in got)
+
+
+def test_binding_refuses_and_leaves_outputs_alone(B):
+    """What the binding checks before the ABI sees it: types, sizes, layouts and numbers that do not fit."""
+    lens, page, hd = [20, 5], 16, 64
+    q, kc, vc, table, start, sc = attn_case(lens, [1, 1], 4, 2, hd, page, FP, FP, "hnd", 3)
+    t, n = ints(table), ints(lens)
+    out = torch.full_like(q, 7.0)
+    z, u, token = torch.zeros((2, 9), device="cuda"), torch.zeros(2, device="cuda"), ints([-5, -5])
+    k, slots = torch.zeros((2, 2, hd), dtype=FP, device="cuda"), ints([0, 1], torch.int64)
+    rope = torch.zeros((32, hd // 2, 2), device="cuda")
+    i = ints([1, 1])
+    big = ints(np.zeros((2, 4)))
+    attend = lambda *a, **kw: B.paged_attention(*a, out=out, **kw)  # noqa: E731
+    draw = lambda *a, **kw: B.sample(*a, token=token, **kw)  # noqa: E731
+    before = kc.view(torch.int16).clone()  # (bits: unused places hold NaN)
+    calls = [lambda: attend(q, kc, vc, t, n, max_len=2 ** 31), lambda: attend(q, kc, vc, t, n, max_rows="1"),
+             lambda: attend(q, kc, vc, t, n, scale="x"), lambda: attend(q, kc, vc, t.long(), n), lambda: attend(q, kc, vc, t[:1], n),
+             lambda: attend(q, kc, vc, t, n.long()), lambda: attend(q, kc, vc.float(), t, n), lambda: attend(q, kc, vc, t, n, row_start=n),
+             lambda: attend(q[..., :32], kc, vc, t, n), lambda: attend(q.to(BF), kc, vc, t, n), lambda: attend(q, kc, vc, t, n.cpu()),
+             lambda: attend(q, kc, vc, t, n, lse=u), lambda: attend(q, kc, vc, t, n, scratch=torch.zeros(16, dtype=torch.uint8, device="cuda")),
+             lambda: draw(z, u.double()), lambda: draw(z, u[:1]), lambda: draw(z.double(), u), lambda: draw(z.t(), u),
+             lambda: draw(z, u, top_k=u), lambda: draw(z, u, temperature=i), lambda: draw(z, u, logprob=u.cpu()),
+             lambda: B.paged_append(k, k, kc, vc, slots.int()), lambda: B.paged_append(k, k.float(), kc, vc, slots),
+             lambda: B.paged_append(k[:, :1], k, kc, vc, slots), lambda: B.paged_append(k, k, kc, vc, slots, rope=rope),
+             lambda: B.paged_append(k, k, kc, vc, slots, q=k.float()), lambda: B.paged_append(k, k, kc, vc, slots, k_scale=u[:1]),
+             lambda: B.page_map(i, i, big, ints(range(8)), ints([0, 8]), 2 ** 31, max_rows=4),
+             lambda: B.page_map(i, i[:1], big, ints(range(8)), ints([0, 8]), 16, max_rows=4),
+             lambda: B.page_map(i, i, big, ints(range(8)), ints([0, 8, 1]).long(), 16, max_rows=4)]
+    for f in calls:
+        with pytest.raises(B.SparskError) as e:
+            f()
+        assert e.value.code == B.EINVAL
+    torch.cuda.synchronize()
+    assert (out == 7).all() and (token == -5).all() and torch.equal(kc.view(torch.int16), before)
+
+
+def test_threads_with_streams_of_their_own(B):
+    """The binding lets go of Python's lock while it launches: calls of several threads stay apart."""
+    from concurrent.futures import ThreadPoolExecutor
+    lens = [700, 33, 1]
+    q, kc, vc, table, start, sc = attn_case(lens, [1] * 3, 8, 2, 128, 16, BF, FP, "nhd", 21)
+    t, n = ints(table), ints(lens)
+    z, u = torch.randn((3, 5000), device="cuda"), torch.rand(3, device="cuda")
+    want, tokens = B.paged_attention(q, kc, vc, t, n), B.sample(z, u)
+    torch.cuda.synchronize()
+
+    def work(_):
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            got = [(B.paged_attention(q, kc, vc, t, n), B.sample(z, u)) for _ in range(40)]
+        s.synchronize()
+        return all(torch.equal(a, want) and torch.equal(b, tokens) for a, b in got)
+
+    with ThreadPoolExecutor(4) as pool:
+        assert all(pool.map(work, range(4)))

@@ -119,3 +119,16 @@ def test_binding_refuses_what_is_not_on_a_gpu():
         with pytest.raises(B.SparskError) as e:
             f()
         assert e.value.code == B.EINVAL
+
+
+def test_binding_refuses_what_is_not_a_tensor():
+    x = torch.zeros((2, 1, 16, 64), dtype=torch.float16)
+    i = torch.zeros(2, dtype=torch.int32)
+    for f in (lambda: B.paged_append([1], x[:, :, 0], x, x, i), lambda: B.paged_attention(x[:, :, 0], None, x, i.view(1, 2), i, out=x[:, :, 0]),
+              lambda: B.page_map(i, i, x, i, i, 16), lambda: B.sample(5, i, token=i),
+              lambda: B.page_map(7, i, x, i, i, 16, seq_len=i, queue=i, row_start=i, row_seq=i, row_pos=i, slot_map=i, status=i)):
+        with pytest.raises(B.SparskError) as e:
+            f()
+        assert e.value.code == B.EINVAL
+    with pytest.raises(TypeError):
+        B._native().sample(x)
