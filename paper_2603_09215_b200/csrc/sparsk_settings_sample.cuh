@@ -18,8 +18,10 @@
 // h are the halves of one word, so an id costs two shared-memory atomics and seven FP64 operations.  Where there are many rows
 // the issue of some forty instructions an id bounds the kernel (without the atomics of h, or without its series, it is 3 %
 // faster), where there is one the five cluster barriers (about 900 cycles each) and the short passes between them.
-// One row of 6,561 ids 15 us, of 151,936 (top-p) 31, 16 of 151,552 in bf16 with settings of every kind 38, 64 of 151,936 65 without and 86 with
-// top-p (all of them fp32).  What was tried: clusters of sixteen 60 for 38 us and 34 for 31; 512 threads a CTA 52 for 46; 64 registers a
+// One row of 6,561 ids 14.6 us, of 151,936 (top-p) 30, 16 of 151,552 in bf16 with settings of every kind 37.7, 64 of 151,936 65 without and 83 with
+// top-p (all of them fp32); 64 rows of both lengths with settings of every kind 73 (82 with min-p's border found by bisection and each
+// row's ids above it added up where the bins already say that it cuts nothing).  What was tried: a bin's ids put in order by counting them into 512
+// parts: 41 us for 38, 85 for 82, its barriers cost what the comparisons do; clusters of sixteen 60 for 38 us and 34 for 31; 512 threads a CTA 52 for 46; 64 registers a
 // thread and twice the warps 96 for 80; rows read anew from the L2 in each pass, without the shared memory for them, in clusters of
 // four: 100,000 cycles a CTA for 60,000, a pass waits for 32 KB in flight an SM.
 #pragma once
@@ -131,6 +133,10 @@ static __global__ void __launch_bounds__(T, 512 / T) settings_sample_kernel(spar
 
     // ---- the row, its largest and smallest logit
     for (int b = tid; b < 2 * ST_BINS; b += T) bin_lo[b] = 0u;
+    if (tid == 0) {  // (a search finds its bin in every case; where it did not, this or an earlier answer would stay inside the arrays)
+        sh.found = sh.found_cnt = sh.found_n = 0;
+        sh.found_mass = 0;
+    }
     uint32_t kmax = 0u, kmin = ~0u;
     {
         constexpr int ES = TYPE == SPARSK_FP32 ? 4 : 2, WIDE = 16 / ES;
@@ -148,16 +154,24 @@ static __global__ void __launch_bounds__(T, 512 / T) settings_sample_kernel(spar
         if (tid < ahead) take(tid, st_load<TYPE>(a.logits, at + tid));
         for (int i = ahead + wide * WIDE + tid; i < mine; i += T) take(i, st_load<TYPE>(a.logits, at + i));
         const uint4 *body = reinterpret_cast<const uint4 *>(src + ahead * ES);
-#pragma unroll 4
-        for (int i = tid; i < wide; i += T) {
-            const uint4 x = body[i];
-            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        constexpr int BATCH = 6;  // (all asked for at once, the last ones too)
+        for (int i0 = tid; i0 < wide; i0 += T * BATCH) {
+            uint4 x[BATCH];
 #pragma unroll
-            for (int k = 0; k < 4; k++) {
-                if (TYPE == SPARSK_FP32) take(ahead + i * 4 + k, w[k]);
-                else {
-                    take(ahead + i * 8 + k * 2, st_widen<TYPE>(w[k] & 0xffffu));
-                    take(ahead + i * 8 + k * 2 + 1, st_widen<TYPE>(w[k] >> 16));
+            for (int q = 0; q < BATCH; q++)
+                if (i0 + q * T < wide) x[q] = body[i0 + q * T];
+#pragma unroll
+            for (int q = 0; q < BATCH; q++) {
+                const int i = i0 + q * T;
+                if (i >= wide) break;
+                const uint32_t w[4] = {x[q].x, x[q].y, x[q].z, x[q].w};
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                    if (TYPE == SPARSK_FP32) take(ahead + i * 4 + k, w[k]);
+                    else {
+                        take(ahead + i * 8 + k * 2, st_widen<TYPE>(w[k] & 0xffffu));
+                        take(ahead + i * 8 + k * 2 + 1, st_widen<TYPE>(w[k] >> 16));
+                    }
                 }
             }
         }
@@ -290,24 +304,30 @@ static __global__ void __launch_bounds__(T, 512 / T) settings_sample_kernel(spar
     // Calls f(key, place in the slice) for the ids with keys from k_lo to k_hi.
     const auto each_of = [&](uint32_t k_lo, uint32_t k_hi, auto f) {
         const auto key_of = [](uint32_t word) { return word ^ ((uint32_t)((int)word >> 31) | 0x80000000u); };  // (0 for what is never drawn)
-        for (int i = tid * 4; i < mine4; i += T * 16) {
-            // sixteen ids at a time, so that their loads do not wait for what f writes
-            uint4 four[4];
+        const auto all = [&](auto hit) {
+            for (int i = tid * 4; i < mine4; i += T * 16) {
+                // sixteen ids at a time, so that their loads do not wait for what f writes
+                uint4 four[4];
 #pragma unroll
-            for (int q = 0; q < 4; q++)
-                four[q] = i + q * T * 4 < mine4 ? *reinterpret_cast<const uint4 *>(slice + i + q * T * 4) : make_uint4(ST_DEAD, ST_DEAD, ST_DEAD, ST_DEAD);
-            uint32_t hits = 0;
+                for (int q = 0; q < 4; q++)
+                    four[q] = i + q * T * 4 < mine4 ? *reinterpret_cast<const uint4 *>(slice + i + q * T * 4) : make_uint4(ST_DEAD, ST_DEAD, ST_DEAD, ST_DEAD);
+                uint32_t hits = 0;
 #pragma unroll
-            for (int q = 0; q < 4; q++) {
-                const uint32_t word[4] = {four[q].x, four[q].y, four[q].z, four[q].w};
+                for (int q = 0; q < 4; q++) {
+                    const uint32_t word[4] = {four[q].x, four[q].y, four[q].z, four[q].w};
 #pragma unroll
-                for (int k = 0; k < 4; k++) hits |= key_of(word[k]) - k_lo <= k_hi - k_lo ? 1u << (q * 4 + k) : 0u;
+                    for (int k = 0; k < 4; k++) if (hit(word[k])) hits |= 1u << (q * 4 + k);
+                }
+                for (; hits; hits &= hits - 1) {
+                    const int k = __ffs(hits) - 1, at = i + (k >> 2) * T * 4 + (k & 3);
+                    f(key_of(slice[at]), at);
+                }
             }
-            for (; hits; hits &= hits - 1) {
-                const int k = __ffs(hits) - 1, at = i + (k >> 2) * T * 4 + (k & 3);
-                f(key_of(slice[at]), at);
-            }
-        }
+        };
+        const uint32_t base = (k_lo & 0x80000000u) ? st_bits(k_lo) : st_bits(k_hi), span = k_hi - k_lo;
+        // (numbers of one sign are a stretch of words, too)
+        if ((int)(k_lo ^ k_hi) < 0) all([&](uint32_t word) { return key_of(word) - k_lo <= span; });
+        else all([&](uint32_t word) { return word - base <= span; });
     };
     // The cluster's bins added up, this CTA's share of them: ids and mass before each; `e` of a bin is what its ids weigh less h / s, `next` of a
     // bin by that of the one before.  What lies beyond a whole row's range weighs nothing.
@@ -443,18 +463,13 @@ static __global__ void __launch_bounds__(T, 512 / T) settings_sample_kernel(spar
         return by == ST_BY_COUNT ? count >= target : by == ST_BY_MASS ? (double)mass >= target : (double)mass > target;
     };
     const auto locate = [&](int by, double target) {
-        int r = 0;
-        while (r < C && !meets(by, target, sh.all_count[r + 1], sh.all_mass[r + 1])) r++;
-        const bool none = r == C;  // (no bin's end meets it, for a rounding's sake: it is the last id's bin)
-        if (none)
-            for (r = C - 1; r > 0 && sh.all_count[r + 1] == sh.all_count[r];) r--;
+        const int l = lane % C;
+        const uint32_t met = __ballot_sync(0xffffffffu, meets(by, target, sh.all_count[l + 1], sh.all_mass[l + 1])) & ((1u << C) - 1u),
+                       any = __ballot_sync(0xffffffffu, sh.all_count[l + 1] > sh.all_count[l]) & ((1u << C) - 1u);
+        const bool none = met == 0u;  // (no bin's end meets it, for a rounding's sake: it is the last id's bin)
+        const int r = none ? 31 - __clz(any | 1u) : __ffs(met) - 1;
         const unsigned long long *masses = Cl::of(own_mass, r), m_here = sh.all_mass[r], m_all = sh.all_mass[r + 1];
         const int *counts = Cl::of(own_count, r), c_here = sh.all_count[r], c_all = sh.all_count[r + 1];
-        if (tid == 0) {  // (found below in every case; whatever is not would stay inside the arrays)
-            sh.found = sh.found_cnt = sh.found_n = 0;
-            sh.found_mass = 0;
-        }
-        __syncthreads();
         for (int b = tid; b < OWN; b += T) {
             const int c0 = c_here + counts[b], c1 = b + 1 < OWN ? c_here + counts[b + 1] : c_all;
             const unsigned long long m0 = m_here + masses[b], m1 = b + 1 < OWN ? m_here + masses[b + 1] : m_all;
@@ -504,8 +519,14 @@ static __global__ void __launch_bounds__(T, 512 / T) settings_sample_kernel(spar
                 keep = 1;
                 continue;
             }
-            // the largest logit that is too light
-            const uint32_t light = last_key([&](uint32_t k) { return exp(log_weight(k)) < (double)min_p; });
+            // The largest logit that is too light: a rounding or two from where the logarithm says, where 32 lanes look at 32 keys
+            const auto heavy = [&](uint32_t k) { return !(exp(log_weight(k)) < (double)min_p); };
+            const uint32_t k0 = max(st_key(__float_as_uint((float)(z0 + log((double)min_p) / inv_t))), 17u) - 16u;
+            const uint32_t heavies = __ballot_sync(0xffffffffu, heavy(min(k0 + lane, top)));
+            const uint32_t light = heavies && !(heavies & 1u) ? min(k0 + __ffs(heavies) - 1, top) - 1u : last_key([&](uint32_t k) { return !heavy(k); });
+            // (nothing to cut where the bins before its own hold all that is left)
+            const int lb = bin_of(place(st_bits(light)));
+            if (!divided && light && sh.all_count[lb / OWN] + *Cl::of(own_count + lb % OWN, lb / OWN) >= keep) continue;
             // ids and mass above it, added up in a fixed order
             int c = 0;
             unsigned long long m = 0;

@@ -452,6 +452,28 @@ def test_sample(B, V, dtype, scale):
     run_sample(B, z, u, T, k, p, m, lo, hi)
 
 
+@pytest.mark.parametrize("V", [100, 20000, 151936])
+@pytest.mark.parametrize("dtype", [torch.float32, BF])
+@pytest.mark.parametrize("shift", [0.0, -500.0, 3000.0])
+def test_sample_light_logits(B, V, dtype, shift):
+    """min-p whose border lies near zero, far from it, behind every id, or before the second one; after cuts that are
+    tighter, and after a bin that had to be divided."""
+    n = 12
+    gen = torch.Generator("cuda").manual_seed(V + 1)
+    z = torch.randn((n, V), generator=gen, device="cuda") * 2.0
+    z -= z.max(1, keepdim=True).values  # (the border at ln(min_p) T is around zero in the rows that are raised by it)
+    m = [1e-30, 1e-6, 0.01, 0.3, 1 - 2.0 ** -24, 1.0, 0.05, 0.05, 1e-3, 1e-3, 0.2, 1e-12]
+    T = [1.0, 0.5, 1.0, 2.0, 1.0, 1.0, 1.0, 1.0, 0.7, 3.0, 1.0, 1.0]
+    for i in (1, 2, 3, 9):
+        z[i] -= T[i] * float(np.log(m[i]))
+    z = z + shift
+    z[11, V // 3:] = z[11, 0]  # so many equal that their bin is divided, or is one number
+    z = z.to(dtype)
+    u = torch.rand(n, generator=gen, device="cuda").clamp(max=1 - 2.0 ** -24).tolist()
+    run_sample(B, z, u, T, None, None, m)
+    run_sample(B, z, u, T, [0, 0, 0, 0, 0, 0, 5, 0, 0, 70, 0, V // 2], [1.0, 1.0, 1.0, 1.0, 1.0, 1.0, 1.0, 0.5, 0.9, 0.9, 0.05, 0.9], m)
+
+
 def test_sample_by_hand(B):
     """Weights that are powers of two, so that every border is exact: the first id beyond u times the kept mass."""
     z = torch.tensor([[-2.0, 0.0, -2.0, -1.0]], device="cuda").expand(8, 4).contiguous() * 0.693147180559945
