@@ -5,7 +5,7 @@
 //   1. Bins of equal width in (max - z) / T, as many as the row's range asks for (40 at most: beyond that even a
 //      quarter of a million ids weigh less than 2^-40 of the whole).  A bin adds up how many ids it holds and what they weigh; the sums of
 //      bins, in order, say in which bin a target lies.
-//   2. The bin's ids (a few hundred at the most, nearly always) are gathered, ranked by counting and added up one by one.  A bin of more ids is
+//   2. The bin's ids (a few hundred at the most, nearly always) are gathered, put in order and added up one by one.  A bin of more ids is
 //      divided again, by the bits of its logits, until few are left or all are equal.
 // Sums do not depend on the order of the additions: all masses are whole numbers of 2^-44, and within a bin the weights
 // are added as whole numbers too.  With x = s (max - z) / T, bin
@@ -18,12 +18,11 @@
 // h are the halves of one word, so an id costs two shared-memory atomics and seven FP64 operations.  Where there are many rows
 // the issue of some forty instructions an id bounds the kernel (without the atomics of h, or without its series, it is 3 %
 // faster), where there is one the five cluster barriers (about 900 cycles each) and the short passes between them.
-// One row of 6,561 ids 14.6 us, of 151,936 (top-p) 30, 16 of 151,552 in bf16 with settings of every kind 37.7, 64 of 151,936 65 without and 83 with
+// One row of 6,561 ids 14.6 us, of 151,936 (top-p) 28.5, 16 of 151,552 in bf16 with settings of every kind 37.7, 64 of 151,936 60 without and 76 with
 // top-p (all of them fp32); 64 rows of both lengths with settings of every kind 73 (82 with min-p's border found by bisection and each
-// row's ids above it added up where the bins already say that it cuts nothing).  What was tried: a bin's ids put in order by counting them into 512
-// parts: 41 us for 38, 85 for 82, its barriers cost what the comparisons do; clusters of sixteen 60 for 38 us and 34 for 31; 512 threads a CTA 52 for 46; 64 registers a
-// thread and twice the warps 96 for 80; rows read anew from the L2 in each pass, without the shared memory for them, in clusters of
-// four: 100,000 cycles a CTA for 60,000, a pass waits for 32 KB in flight an SM.
+// row's ids above it added up where the bins already say that it cuts nothing).  What was tried: clusters of sixteen 60 for 38 us
+// and 34 for 31; 512 threads a CTA 52 for 46; 64 registers a thread and twice the warps 96 for 80; rows read anew from the L2 in each
+// pass, without the shared memory for them, in clusters of four: 100,000 cycles a CTA for 60,000, a pass waits for 32 KB in flight an SM.
 #pragma once
 
 #include <cooperative_groups.h>
@@ -63,7 +62,12 @@ __device__ __forceinline__ double st_double(uint32_t bits)
 
 constexpr int ST_MAX_WARPS = 16;
 constexpr int ST_BINS = 2048;   // the last one holds what lies beyond the range
-constexpr int ST_FEW = 512;     // ids that are ranked by counting
+constexpr int ST_FEW_LOG = 9;
+constexpr int ST_FEW = 1 << ST_FEW_LOG;  // ids that are put in order
+// Up to so many by comparing each with all, more by counting them into parts, whose barriers take what 130 comparisons a thread take.  64 rows of
+// 151,936 fp32 ids with top-p: 84 us by comparing alone, 76 like this (81 from 256 ids on); rows with settings of every kind, mostly few
+// ids: 73 like this, 79 by parts alone.
+constexpr int ST_COMPARED = 128;
 constexpr double ST_RANGE = 40;
 constexpr double ST_UNIT = 17592186044416.0;  // 2^44 units of mass are the largest weight (2^18 ids of it fit 64 bits)
 constexpr uint32_t ST_DEAD = 0xffffffffu;
@@ -111,12 +115,16 @@ static __global__ void __launch_bounds__(T, 512 / T) settings_sample_kernel(spar
 {
     typedef StCluster<C> Cl;
     constexpr int WARPS = T / 32, OWN = ST_BINS / C, PER = OWN > T ? OWN / T : 1;  // bins a CTA, a thread adds up
-    constexpr int EACH = ST_FEW / T;  // ids to rank, a thread
+    constexpr int EACH = ST_FEW / T;  // ids to put in order, a thread
+    constexpr int GRAIN = TYPE == SPARSK_BF16 ? 16 : TYPE == SPARSK_FP16 ? 13 : 0;  // different keys are 2^GRAIN apart at least
     extern __shared__ __align__(16) unsigned char st_smem[];
     uint32_t *bin_lo = reinterpret_cast<uint32_t *>(st_smem), *bin_hi = bin_lo + ST_BINS;
     // ranked ids and their masses take the bins' place when these have been added up
     unsigned long long *ranked = reinterpret_cast<unsigned long long *>(st_smem);
     unsigned long long *ranked_mass = reinterpret_cast<unsigned long long *>(st_smem + ST_FEW * 8);
+    unsigned long long *staged = reinterpret_cast<unsigned long long *>(st_smem + ST_FEW * 16);
+    int *part_n = reinterpret_cast<int *>(st_smem + ST_FEW * 24), *part_at = part_n + ST_FEW;
+    static_assert(ST_FEW * 32 <= ST_BINS * 8, "all of them in the bins' place");
     unsigned long long *own_mass = reinterpret_cast<unsigned long long *>(st_smem + ST_BINS * 8);  // before each of this CTA's bins
     int *own_count = reinterpret_cast<int *>(own_mass + OWN);
     uint32_t *slice = reinterpret_cast<uint32_t *>(own_count + OWN);
@@ -602,8 +610,9 @@ static __global__ void __launch_bounds__(T, 512 / T) settings_sample_kernel(spar
                 __syncthreads();
             }
             if (in <= ST_FEW) {
-                // gathered, ranked by counting, and added up
+                // gathered, put in order, and added up
                 if (tid == 0) sh.list_n[turn] = 0;
+                for (int b = tid; b < ST_FEW; b += T) part_n[b] = 0;
                 __syncthreads();
                 each_of(k_lo, k_hi, [&](uint32_t k, int i) {
                     const int at = atomicAdd(&sh.list_n[turn], 1);
@@ -627,26 +636,71 @@ static __global__ void __launch_bounds__(T, 512 / T) settings_sample_kernel(spar
                 }
                 turn ^= 1;
                 have = min(have, ST_FEW);
+                if (have <= ST_COMPARED) {
+                    // each compared with all
 #pragma unroll
-                for (int q = 0; q < EACH; q++) ranked[tid + q * T] = me[q];
-                __syncthreads();
-                int place_of[EACH] = {};
-                if (have > T) {
-#pragma unroll 4
-                    for (int j = 0; j < have; j++) {
-                        const unsigned long long other = ranked[j];
-#pragma unroll
-                        for (int q = 0; q < EACH; q++) place_of[q] += other < me[q] ? 1 : 0;
-                    }
-                } else if (warp * 32 < have) {
+                    for (int q = 0; q < EACH; q++) ranked[tid + q * T] = me[q];
+                    __syncthreads();
+                    int place_of = 0;
+                    if (warp * 32 < have) {
 #pragma unroll 8
-                    for (int j = 0; j < have; j++) place_of[0] += ranked[j] < me[0] ? 1 : 0;
-                }
-                __syncthreads();
+                        for (int j = 0; j < have; j++) place_of += ranked[j] < me[0] ? 1 : 0;
+                    }
+                    __syncthreads();
+                    if (tid < have) ranked[place_of] = me[0];
+                    __syncthreads();
+                } else {
+                    // ST_FEW parts of the keys' stretch (a part a key, or several parts by ids where it has few keys, as with
+                    // logits of 16 bits), counted, and each put in order by itself
+                    const uint32_t span = k_hi - k_lo, values = (span >> GRAIN) + 1u;
+                    const int per_value = values <= ST_FEW ? ST_FEW / (int)values : 0, shift = max(0, 32 - __clz(span) - ST_FEW_LOG);
+                    const float by_id = (float)per_value / (float)n;
+                    const auto part_of = [&](unsigned long long it) {
+                        const uint32_t off = k_hi - ~(uint32_t)(it >> 32);
+                        if (per_value) return (int)(off >> GRAIN) * per_value + min((int)((float)(uint32_t)it * by_id), per_value - 1);
+                        return (int)(off >> shift);
+                    };
+                    int part[EACH], at_part[EACH];
 #pragma unroll
-                for (int q = 0; q < EACH; q++)
-                    if (tid + q * T < have) ranked[place_of[q]] = me[q];
-                __syncthreads();
+                    for (int q = 0; q < EACH; q++)
+                        if (tid + q * T < have) {
+                            part[q] = part_of(me[q]);
+                            at_part[q] = atomicAdd(part_n + part[q], 1);
+                        }
+                    __syncthreads();
+                    int p_n[EACH], p_all = 0;
+#pragma unroll
+                    for (int q = 0; q < EACH; q++) p_all += p_n[q] = part_n[tid * EACH + q];
+                    int p_at = p_all;
+#pragma unroll
+                    for (int o = 1; o < 32; o <<= 1) {
+                        const int x = __shfl_up_sync(0xffffffffu, p_at, o);
+                        if (lane >= o) p_at += x;
+                    }
+                    if (lane == 31) sh.wcnt[warp] = p_at;
+                    __syncthreads();
+                    p_at -= p_all;
+                    for (int w = 0; w < warp; w++) p_at += sh.wcnt[w];
+#pragma unroll
+                    for (int q = 0; q < EACH; q++) {
+                        part_at[tid * EACH + q] = p_at;
+                        p_at += p_n[q];
+                    }
+                    __syncthreads();
+#pragma unroll
+                    for (int q = 0; q < EACH; q++)
+                        if (tid + q * T < have) staged[part_at[part[q]] + at_part[q]] = me[q];
+                    __syncthreads();
+#pragma unroll
+                    for (int q = 0; q < EACH; q++)
+                        if (tid + q * T < have) {
+                            const int first = part_at[part[q]], end = first + part_n[part[q]];
+                            int place_of = first;
+                            for (int j = first; j < end; j++) place_of += staged[j] < me[q] ? 1 : 0;
+                            ranked[place_of] = me[q];
+                        }
+                    __syncthreads();
+                }
                 unsigned long long m[EACH], all = 0;
 #pragma unroll
                 for (int q = 0; q < EACH; q++) {
