@@ -180,8 +180,9 @@ static __global__ void __launch_bounds__(PM_THREADS) page_map_kernel(const PageM
 // A thread takes eight pairs (j, j + head_dim / 2) of one head of one row: two 16-byte reads and two writes of a
 // 16-bit type, and the pairs' cosines and sines once.  Bound by bytes where there are many rows (every number is
 // read and written once), by latency in a decode step.  4,001 rows of 36 heads of 128 (bf16, 32 of them queries, into e4m3 pages): 74 MB
-// in 20.9 us.  Four heads a thread, turned by the same factors: 20.7, two: 21.9; numbers asked for only when it was known
-// where they go: 23.4.
+// in 20.9 us (torch's copy of as many bytes: 26).  Four heads a thread, turned by the same factors: 20.7, two: 21.9; numbers asked
+// for only when it was known where they go: 23.4.  Rows that do not start at 16 bytes, rising positions: 21 us for 17.7, fp32
+// 28 (read number by number 23 and 33).
 constexpr int PA_THREADS = 256;
 
 // A number beyond the type's largest is stored as that (an infinity in the cache would make every later score
@@ -232,13 +233,24 @@ struct PaRaw {
                 const uint4 x = p[i];
                 w[i * 4] = x.x; w[i * 4 + 1] = x.y; w[i * 4 + 2] = x.z; w[i * 4 + 3] = x.w;
             }
-        } else if constexpr (TYPE == SPARSK_FP32) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) w[i] = reinterpret_cast<const uint32_t *>(base)[at + i];
         } else {
-            const uint16_t *p = reinterpret_cast<const uint16_t *>(base) + at;
+            // The 16-byte blocks that they lie in (each holds a byte of them, so none is read that the row has no part in), put
+            // together by shifts.
+            const char *p = reinterpret_cast<const char *>(base) + at * (TYPE == SPARSK_FP32 ? 4 : 2);
+            const unsigned m = (unsigned)((uintptr_t)p & 15);
+            const uint4 *b = reinterpret_cast<const uint4 *>(p - m);
+            uint32_t x[N + 4];
 #pragma unroll
-            for (int i = 0; i < 4; i++) w[i] = (uint32_t)p[i * 2] | ((uint32_t)p[i * 2 + 1] << 16);
+            for (int i = 0; i <= N / 4; i++) {
+                const uint4 y = i < N / 4 || m ? b[i] : make_uint4(0u, 0u, 0u, 0u);
+                x[i * 4] = y.x; x[i * 4 + 1] = y.y; x[i * 4 + 2] = y.z; x[i * 4 + 3] = y.w;
+            }
+#pragma unroll
+            for (int i = 0; i < N + 2; i++) x[i] = m & 8 ? x[i + 2] : x[i];
+#pragma unroll
+            for (int i = 0; i < N + 1; i++) x[i] = m & 4 ? x[i + 1] : x[i];
+#pragma unroll
+            for (int i = 0; i < N; i++) w[i] = TYPE == SPARSK_FP32 ? x[i] : __funnelshift_r(x[i], x[i + 1], (m & 2) * 8);
         }
     }
     __device__ __forceinline__ void floats(float (&v)[8]) const

@@ -189,6 +189,28 @@ def test_append(B, n, hq, hk, hd, page, x, cache, layout, turn, shift):
         assert near(got[on], qt[on], qo_type, 3 * 2.0 ** -24 * slack[on]).all() and (got[~on] == 3.0).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("shift", range(8))
+def test_append_rows_at_every_offset(B, dtype, shift):
+    """Rows that start at any number of a 16-byte block, the last one at its memory's end: the same as from aligned rows."""
+    n, hq, hk, hd, page = 9, 3, 2, 64, 16
+    gen = torch.Generator("cuda").manual_seed(shift)
+    w = (hq + 2 * hk) * hd
+    x = torch.randn((n, w), generator=gen, device="cuda").to(dtype)
+    for gap in (0, 1, 8):
+        flat = torch.full((shift + n * (w + gap) - gap,), float("nan"), dtype=dtype, device="cuda")
+        rows = flat.as_strided((n, w), (w + gap, 1), shift)
+        rows.copy_(x)
+        got = []
+        for y in (x, rows):
+            q, k, v = (t.unflatten(1, (-1, hd)) for t in (y[:, :hq * hd], y[:, hq * hd:(hq + hk) * hd], y[:, (hq + hk) * hd:]))
+            kc, vc = (torch.zeros((2, hk, page, hd), dtype=FP, device="cuda") for _ in range(2))
+            out = B.paged_append(k, v, kc, vc, ints(range(n), torch.int64), q=q, row_pos=ints(range(n)),
+                                 rope=torch.arange(n * hd, dtype=torch.float32, device="cuda").view(n, hd // 2, 2) / 100)
+            got.append((out, kc, vc))
+        assert all(torch.equal(a, b) and not a.isnan().any() for a, b in zip(*got))
+
+
 def test_append_not_finite_and_in_place(B):
     gen = torch.Generator("cuda").manual_seed(0)
     for cache in (torch.float16, torch.bfloat16, torch.float8_e4m3fn):
