@@ -6,7 +6,6 @@
 // links against torch alone.
 #include <Python.h>
 
-#include <algorithm>
 #include <cstdint>
 #include <exception>
 #include <string>
@@ -120,7 +119,10 @@ int32_t *table(PyObject *o, int64_t n, int dev, int64_t &stride, int32_t &blocks
     same_device(t, dev, "block_table");
     if (t.scalar_type() != at::kInt || t.dim() != 2 || t.size(0) < n || (t.size(1) > 1 && t.stride(1) != 1))
         refuse("block_table: int32 [sequences, blocks], a row's entries contiguous");
-    stride = std::max(t.stride(0), t.size(1));  // (of a table of one row the stride says nothing)
+    // (where one row is read its stride says nothing; rows that share memory, as expanded ones do, have no place of their own
+    // for the pages that a step enters, and no distance that the ABI takes)
+    if (n > 1 && t.stride(0) < t.size(1)) refuse("block_table: rows that do not overlap are wanted");
+    stride = n > 1 ? t.stride(0) : t.size(1);
     blocks = size(t.size(1), "blocks");
     return static_cast<int32_t *>(t.data_ptr());
 }

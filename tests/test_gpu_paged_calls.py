@@ -1,0 +1,45 @@
+"""Calls of the paged operators that their documentation allows, or that have to be refused, and that can go wrong in ways of their
+own (references in 64 bits: tests/paged_util.py)."""
+import numpy as np
+import pytest
+import torch
+
+from tests import paged_util as pu
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a CUDA device")
+    from paper_2603_09215_b200 import binding
+    return binding
+
+
+def ints(v, dtype=torch.int32):
+    return torch.tensor(np.asarray(v), dtype=dtype, device="cuda")
+
+
+BF, FP, E4 = torch.bfloat16, torch.float16, torch.float8_e4m3fn
+
+
+def test_tables_whose_rows_overlap_are_refused(B):
+    """An expanded table, and one whose rows begin inside one another: there is no row of its own for every sequence.  Of a table of one
+    row the stride says nothing."""
+    n, blocks, page = 3, 4, 16
+    kc = torch.zeros((8, 2, page, 64), dtype=FP, device="cuda")
+    q, lens = torch.zeros((n, 4, 64), dtype=FP, device="cuda"), ints([40, 50, 64])
+    flat = ints(range(7))
+    for table in (flat[:blocks].view(1, blocks).expand(n, blocks), flat.as_strided((n, blocks), (1, 1))):
+        out = torch.full_like(q, 7.0)
+        ring, queue = ints(range(8)), ints([0, 8])
+        for call in (lambda: B.paged_attention(q, kc, kc, table, lens, out=out),
+                     lambda: B.page_map(lens, ints([1] * n), table, ring, queue, page, max_rows=8)):
+            with pytest.raises(B.SparskError) as e:
+                call()
+            assert e.value.code == B.EINVAL
+        torch.cuda.synchronize()
+        assert (out == 7).all() and flat.tolist() == list(range(7)) and ring.tolist() == list(range(8))
+        one = B.paged_attention(q[:1], kc, kc, table[:1], lens[:1])
+        assert (one == 0).all()
