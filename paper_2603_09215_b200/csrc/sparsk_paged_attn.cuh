@@ -199,7 +199,8 @@ __device__ __forceinline__ bool pt_clean(unsigned char *V, int p0, int end, int 
             }
         }
     }
-    return __any_sync(0xffffffffu, odd);  // (also: the cleared rows are written)
+    __syncwarp();  // the warp's other lanes read the cleared rows (a vote orders no memory)
+    return __any_sync(0xffffffffu, odd);
 }
 
 // O += P V for one box.  ODD: numbers that are not finite are left out of the products and given one by one to the vectors

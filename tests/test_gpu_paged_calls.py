@@ -43,3 +43,27 @@ def test_tables_whose_rows_overlap_are_refused(B):
         assert (out == 7).all() and flat.tolist() == list(range(7)) and ring.tolist() == list(range(8))
         one = B.paged_attention(q[:1], kc, kc, table[:1], lens[:1])
         assert (one == 0).all()
+
+
+@pytest.mark.parametrize("cache,hd", [(FP, 64), (FP, 128), (BF, 128), (E4, 64), (E4, 128)])
+def test_what_lies_behind_every_end_is_cleared(B, cache, hd):
+    """Hundreds of segments, each with an end inside a box of 16 positions behind which lie NaN: cleared by some of a warp's lanes,
+    read by others.  Whatever lies there, the bits of the result are the same, every time."""
+    n, hq, hk, page = 256, 8, 2, 16
+    gen = torch.Generator("cuda").manual_seed(hd)
+    lens = [1 + (i * 7) % 47 for i in range(n)]
+    blocks = 3
+    table = torch.randperm(n * blocks, generator=gen, device="cuda").to(torch.int32).view(n, blocks)
+    kc, vc = (torch.randn((n * blocks, hk, page, hd), generator=gen, device="cuda") for _ in "kv")
+    q = torch.randn((n, hq, hd), generator=gen, device="cuda").to(BF)
+    behind = torch.arange(blocks * page, device="cuda")[None] >= ints(lens)[:, None]  # [sequence, position]
+    place = (table.long()[:, :, None] * page + torch.arange(page, device="cuda")).view(n, -1)[behind]
+    want = None
+    for fill in (0.0, float("nan"), 3.0, float("nan")):
+        for c in (kc, vc):
+            c[place // page, :, place % page] = fill
+        k8, v8 = kc.to(cache), vc.to(cache)
+        for _ in range(5):
+            got = B.paged_attention(q, k8, v8, table, ints(lens))
+            want = got if want is None else want
+            assert torch.equal(got, want) and not bool(got.isnan().any())
