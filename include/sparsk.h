@@ -390,7 +390,9 @@ int sparsk_paged_append(const sparsk_paged_append_args *args /*host*/, void *cud
  * were.  Positions that a row does not see, and what lies behind a sequence's end in its last page, may hold anything, infinities and
  * NaN too.  Positions in a page whose id is outside [0, n_pages) are left out; a length beyond the table is
  * cut at the table's end.  Scores, softmax and sums are held in fp32; queries meet fp16 and e4m3 pages as fp16 numbers (of magnitude
- * 65,504 at most), bf16 pages as bf16 numbers.
+ * 65,504 at most), bf16 pages as bf16 numbers.  A weight meets the values as one fp16 number (2^-11 of itself off at most), or, where
+ * queries are fp16 or pages bf16, as two of the pages' 16-bit type (2^-16); fp16 weights are further off by up to 2^-20 of the largest
+ * among the same 16 positions of a page, however far that lies below the row's maximum (e^-52 at most).
  * max_rows and max_len are what the caller knows of a sequence's most rows and largest length (0: nothing): they size the launch, results do
  * not depend on them.  `scratch` (device, 256-byte aligned, >= sparsk_paged_attention_scratch_bytes) is overwritten;
  * nothing in it needs clearing; two calls that may overlap on the GPU need scratch of their own.

@@ -160,6 +160,7 @@ extern "C" int sparsk_paged_attention(const sparsk_paged_attn_args *a, void *scr
     p.q_row_stride = a->q_row_stride; p.q_head_stride = a->q_head_stride;
     p.out_row_stride = a->out_row_stride; p.out_head_stride = a->out_head_stride;
     p.scale_log2 = (a->scale > 0.f ? a->scale : 1.f / sqrtf((float)a->pool.head_dim)) * 1.4426950408889634f;
+    p.up = a->pool.type == SPARSK_BF16 ? 0.f : PT_UP;
     p.q_type = a->q_type; p.n_rows = a->n_rows; p.n_seqs = a->n_seqs; p.max_blocks = a->max_blocks;
     p.page_size = a->pool.page_size; p.n_pages = a->pool.n_pages;
     p.Hk = a->pool.n_kv_heads; p.G = a->n_q_heads / a->pool.n_kv_heads;

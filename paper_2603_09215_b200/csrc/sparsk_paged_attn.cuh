@@ -43,7 +43,9 @@ constexpr int PT_END_COST = 24;                // a segment's set-up and end, in
 constexpr int PT_WHOLE = 8;                    // a segment of up to so many boxes is never cut
 constexpr int PT_MIN_SHARE = 20;               // the same unit (40 puts two short segments into one share: 7.1 us for 5.1; one of 1,500
                                                // positions 11.2 us, with 40 13.1, with 80 16.5)
-constexpr float PT_LAG = 8.f;                  // in powers of two
+constexpr float PT_LAG = 8.f;                  // in powers of two, and these
+constexpr float PT_UP = 7.f;                   // weights that are fp16 numbers lie so much higher: 2^15 at most
+constexpr float PT_DEEP = 12.f, PT_LIFT = 64.f; // a box whose largest weight is below 2^-PT_DEEP is raised further, 2^PT_LIFT at most
 constexpr int PT_RING_BYTES = 112 * 1024;      // of a CTA's shared memory: boxes, queries, sums that meet
 constexpr int PJ_THREADS = 256;
 
@@ -70,6 +72,7 @@ struct PtArgs {
     float2 *part_ml;    // [shares][2][tiles][16]: maximum in powers of two, sum
     long long table_stride, q_row_stride, q_head_stride, out_row_stride, out_head_stride;
     float scale_log2;
+    float up;           // PtForm::UP
     int q_type, n_rows, n_seqs, max_blocks, page_size, n_pages, Hk, G;
     int tiles;          // of 16 query vectors, in a segment at most (1, 2 or 4)
     int page_shift;     // a page has 2^page_shift boxes, or -1
@@ -93,6 +96,7 @@ struct PtForm {
     // (every box to every warp).  48 refresh blocks over e4m3 / fp16 pages, us: 2, 3, 5 47.2 / 41.3; 2, 3, 6 50.1 / 43.5; 2, 3, 8 56.6 / 49.9; 2,
     // 2, 5 56.5 / 48.4; 2, 4, 6 48.9 / 43.7 (and 28 vectors in fp16 56.1 for 51.9).
     static constexpr int PT_C2 = 3, PT_C4 = 5;
+    static constexpr float UP = CT == SPARSK_BF16 ? 0.f : PT_UP;  // (bf16 weights have the range of fp32)
     __device__ __forceinline__ static int box_cost(int vectors) { return vectors <= 16 ? 2 : vectors <= 32 ? PT_C2 : PT_C4; }
     // byte offset of 16-byte chunk c of row r inside a box
     __device__ __forceinline__ static int at(int r, int c)
@@ -125,6 +129,8 @@ __device__ __forceinline__ void pt_mma(float (&d)[4], const uint32_t (&a)[4], ui
     if (CT == SPARSK_BF16) mma_bf16(d, a, b0, b1);
     else mma_f16(d, a, b0, b1);
 }
+// 2^n, exactly (exp2f is not)
+__device__ __forceinline__ float pt_power(int n) { return __int_as_float((127 + n) << 23); }
 // two e4m3 numbers -> two fp16 numbers (exact)
 __device__ __forceinline__ uint32_t pt_widen(uint32_t two)
 {
@@ -592,7 +598,9 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
     const int t4 = lane & 3;
     int mt = 0, pg = 0, PG = 1;  // this warp's tile of 16 vectors, its place among the PG warps of the tile
     uint32_t qa[KS][4];
-    float o[NT][4], m_run[2], l_run[2], c_log2 = 0.f;
+    // of a vector: its maximum, what its weights are taken relative to, the middle of the maxima that a box may have without
+    // scaling, and how far they may lie from it
+    float o[NT][4], m_run[2], m_use[2], m_mid[2], m_far[2], l_run[2], c_log2 = 0.f;
     // where this lane reads its rows of a box: the chunk's low bit is the lane's, even steps turn the others
     const int k_at = F::at((lane & 7) + ((lane >> 4) << 3), (lane >> 3) & 1), v_at = F::at((lane & 7) + ((lane >> 3) & 1) * 8, lane >> 4);
     int limit[2], lim_min = 0, meetings = 0, segs = 0;
@@ -626,8 +634,9 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
             for (int hf = 0; hf < 2; hf++) {
                 const int v = v0 + (lane >> 2) + hf * 8;
                 const bool have = v < n_vec;
-                m_run[hf] = -INFINITY;
-                l_run[hf] = 0.f;
+                m_run[hf] = m_mid[hf] = -INFINITY;
+                m_use[hf] = l_run[hf] = 0.f;
+                m_far[hf] = !have ? INFINITY : F::UP > 0.f ? (PT_LAG + PT_DEEP) / 2 : PT_LAG;
                 limit[hf] = have ? d.len - d.rows + pt_row_of(a, v) : -1;  // the last position that this vector sees
             }
             // (the rows of vectors that a tile does not have hold anything, and nobody reads what comes of them)
@@ -708,12 +717,32 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
             // Weights are taken relative to a maximum that follows the true one only when that has grown by more than
             // 2^PT_LAG: up to there they fit fp16 as well, and what was summed before needs no rescaling (which almost every box
             // would ask for otherwise: it is enough that one of sixteen vectors meets a larger score).
-            if (__any_sync(0xffffffffu, top[0] > m_run[0] + PT_LAG || top[1] > m_run[1] + PT_LAG)) {
+            // fp16 ends at 2^-24 and has all its bits from 2^-14 on, and many light positions can outweigh a heavy one whose values
+            // are near zero.  So weights are 2^UP times what they are, and those of a box that holds none above 2^-PT_DEEP (of
+            // the maximum) are raised by a power of two of their own, for which the sums are raised before the products and
+            // let down after them (exactly): a weight is right to its rounding and 2^-20 of the largest of its box.  (Left as they
+            // were, 32,768 positions e^-17 below one of zero values came out 44 % too large.)
+            float m_box[2] = {m_use[0], m_use[1]};
+            int lift[2] = {0, 0};
+            bool lifted = false;
+            const auto stays = [&](int hf) {  // (true where there is nothing yet and nothing comes: a difference of infinities)
+                const float off = top[hf] - m_mid[hf];
+                return !((F::UP > 0.f ? fabsf(off) : off) > m_far[hf]);
+            };
+            if (!__all_sync(0xffffffffu, stays(0) && stays(1))) {
 #pragma unroll
                 for (int hf = 0; hf < 2; hf++) {
-                    const float m_new = top[hf] > m_run[hf] + PT_LAG ? top[hf] : m_run[hf];  // (each vector by its own scores alone)
-                    const float alpha = m_new == m_run[hf] ? 1.f : exp2f(m_run[hf] - m_new);  // 2^-inf = 0 at first
-                    m_run[hf] = m_new;
+                    float alpha = 1.f;
+                    if (top[hf] > m_run[hf] + PT_LAG) {  // (each vector by its own scores alone)
+                        alpha = exp2f(m_run[hf] - top[hf]);  // 2^-inf = 0 at first
+                        m_run[hf] = top[hf];
+                        m_box[hf] = m_use[hf] = top[hf] - F::UP;
+                        m_mid[hf] = top[hf] - (F::UP > 0.f ? (PT_DEEP - PT_LAG) / 2 : 0.f);
+                    } else if (!stays(hf) && top[hf] != -INFINITY) {
+                        lift[hf] = (int)fminf(m_run[hf] - top[hf], PT_LIFT);
+                        alpha = pt_power(lift[hf]);
+                        m_box[hf] = m_use[hf] - (float)lift[hf];
+                    }
                     l_run[hf] *= alpha;
 #pragma unroll
                     for (int nt = 0; nt < NT; nt++) {
@@ -721,14 +750,14 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
                         o[nt][hf * 2 + 1] *= alpha;
                     }
                 }
+                if (F::UP > 0.f) lifted = __any_sync(0xffffffffu, (lift[0] | lift[1]) != 0);
             }
             uint32_t pa[4], pr[4];
 #pragma unroll
             for (int hf = 0; hf < 2; hf++) {
-                const float m = m_run[hf] == -INFINITY ? 0.f : m_run[hf];  // nothing seen yet: every weight is 2^-inf = 0
                 float w[4];
 #pragma unroll
-                for (int i = 0; i < 4; i++) w[i] = exp2f(v[hf][i] - m);
+                for (int i = 0; i < 4; i++) w[i] = exp2f(v[hf][i] - m_box[hf]);  // (nothing seen yet: 2^-inf = 0)
                 l_run[hf] += (w[0] + w[1]) + (w[2] + w[3]);  // a lane's own positions; lanes are summed at the end
                 pa[hf] = pt_pack2<CT>(w[0], w[1]);
                 pa[2 + hf] = pt_pack2<CT>(w[2], w[3]);
@@ -742,6 +771,18 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
             if (!whole) odd = pt_clean<HD, CT>(const_cast<unsigned char *>(V), p0, d.end, lim_min, lane, wrote);
             if (__builtin_expect(odd, 0)) pt_values<HD, CT, P2, true>(o, pa, pr, V, v_at, lane, p0, d.end, limit);
             else pt_values<HD, CT, P2, false>(o, pa, pr, V, v_at, lane, p0, d.end, limit);
+            if (F::UP > 0.f && lifted) {
+#pragma unroll
+                for (int hf = 0; hf < 2; hf++) {
+                    const float down = pt_power(-lift[hf]);
+                    l_run[hf] *= down;
+#pragma unroll
+                    for (int nt = 0; nt < NT; nt++) {
+                        o[nt][hf * 2] *= down;
+                        o[nt][hf * 2 + 1] *= down;
+                    }
+                }
+            }
         }
         const auto release = [&]() {
             __syncwarp();
@@ -814,7 +855,7 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
                     if (part) a.part_ml[cell * 16 + (lane >> 2) + hf * 8] = make_float2(m[hf], l[hf]);
                     else if (a.lse && have[hf]) {
                         const int v = v0 + (lane >> 2) + hf * 8, r = pt_row_of(a, v);
-                        a.lse[(long long)(d.row0 + r) * a.Hk * a.G + d.head * a.G + v - r * a.G] = l[hf] == 0.f ? -INFINITY : (m[hf] + log2f(l[hf])) * LN2;
+                        a.lse[(long long)(d.row0 + r) * a.Hk * a.G + d.head * a.G + v - r * a.G] = l[hf] == 0.f ? -INFINITY : (m[hf] + (log2f(l[hf]) - F::UP)) * LN2;
                     }
                 }
             }
@@ -964,7 +1005,7 @@ static __global__ void __launch_bounds__(PJ_THREADS) paged_join_kernel(const PtA
             float m = -INFINITY;
 #pragma unroll
             for (int i = 0; i < PER; i++) m = fmaxf(m, red[i][vec]);
-            a.lse[(long long)(row0 + r) * a.Hk * a.G + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+            a.lse[(long long)(row0 + r) * a.Hk * a.G + h] = l == 0.f ? -INFINITY : (m + (log2f(l) - a.up)) * LN2;
         }
     }
 }

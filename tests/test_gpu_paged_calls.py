@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from tests import paged_util as pu
+from tests import test_gpu_paged as base
 
 pytestmark = pytest.mark.gpu
 
@@ -67,3 +67,23 @@ def test_what_lies_behind_every_end_is_cleared(B, cache, hd):
             got = B.paged_attention(q, k8, v8, table, ints(lens))
             want = got if want is None else want
             assert torch.equal(got, want) and not bool(got.isnan().any())
+
+
+@pytest.mark.parametrize("gap", [9.0, 17.0, 20.0, 30.0, 60.0])
+@pytest.mark.parametrize("qt,cache", base.TYPES)
+def test_light_positions_behind_a_sink(B, qt, cache, gap):
+    """The first position's score lies `gap` above the others', those of the next box half as far, and what both boxes hold is zero:
+    the output is what the light positions say, however light.  (Nothing of the sink's box counts, so that every weight that does is off
+    by its rounding, 2^-11, which base.check_attn allows, and 16 of them by 16 times 2^-20 of their largest.)"""
+    lens, rows, page, hd = [3000, 40, 700, 33], [1, 2, 1, 1], 16, 64
+    q, kc, vc, table, start, _ = base.attn_case(lens, rows, 8, 2, hd, page, qt, cache, "hnd", int(gap))
+    q /= 4.0 if cache != E4 else 64.0  # (8-bit pages hold numbers sixteen times as large)
+    q[..., 0] = gap / 64 * hd ** 0.5
+    kc[..., 0] = torch.where(kc[..., 0].float().isnan(), kc[..., 0].float(), 0.0).to(cache)
+    for i in range(len(lens)):
+        first, second = (kc[int(table[i, b])] for b in (0, 1))
+        first[:, 0] = 0.0
+        first[:, 0, 0], second[:, 0, 0] = 64.0, 32.0
+        vc[int(table[i, 0])], vc[int(table[i, 1])] = 0.0, 0.0
+    base.check_attn(B, q, kc, vc, table, lens, start, [None, None], max_rows=2, max_len=3000)
+    base.check_attn(B, q, kc, vc, table, lens, start, [None, None])
