@@ -396,7 +396,11 @@ int sparsk_paged_append(const sparsk_paged_append_args *args /*host*/, void *cud
  * max_rows and max_len are what the caller knows of a sequence's most rows and largest length (0: nothing): they size the launch, results do
  * not depend on them.  `scratch` (device, 256-byte aligned, >= sparsk_paged_attention_scratch_bytes) is overwritten;
  * nothing in it needs clearing; two calls that may overlap on the GPU need scratch of their own.
+ * Every wait inside the kernel is bounded (two seconds: a GPU taken away from it for so long).  Where one runs out, the rows that it
+ * left unfinished get NaN, in lse too, *status (may be NULL) gets the bit SPARSK_PAGED_TIMEOUT, and the call ends.  Bits are only
+ * set, never cleared: one word serves the layers of a step, and the caller clears it.
  * SPARSK_EINVAL for NULL or misaligned pointers, sizes, types or strides out of range. */
+#define SPARSK_PAGED_TIMEOUT 1
 typedef struct {
     sparsk_page_pool pool;
     const void *q;              /* [n_rows][n_q_heads][head_dim] of q_type (bf16; fp16 unless the pool is bf16), turned */
@@ -409,6 +413,8 @@ typedef struct {
     int64_t q_row_stride, q_head_stride, out_row_stride, out_head_stride; /* in elements         */
     int32_t q_type, n_rows, n_seqs, max_blocks, n_q_heads, max_rows, max_len;
     float scale;                /* 0: 1 / sqrt(head_dim)                                         */
+    int32_t *status;            /* [1] or NULL                                                   */
+    int32_t inject_short_copy;  /* test hook, 0 in use; n: the nth CTA waits for bytes that do not come, until its waits run out */
 } sparsk_paged_attn_args;
 size_t sparsk_paged_attention_scratch_bytes(const sparsk_paged_attn_args *args /*host*/);
 int sparsk_paged_attention(const sparsk_paged_attn_args *args /*host*/, void *scratch /*device*/, size_t scratch_bytes,

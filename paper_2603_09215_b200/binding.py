@@ -60,6 +60,7 @@ class Weights(C.Structure):
 
 FP32, BF16, FP16, E4M3 = 0, 1, 2, 3
 PAGES_SHORT, PAGES_TABLE, PAGES_ROWS, PAGES_BAD = 1, 2, 4, 8
+PAGED_TIMEOUT = 1
 
 
 class PageMapArgs(C.Structure):
@@ -85,7 +86,7 @@ class PagedAttnArgs(C.Structure):
     _fields_ = [("pool", PagePool)] + [(n, C.c_void_p) for n in ("q", "out", "lse", "block_table", "seq_len", "row_start")] + [
         (n, C.c_int64) for n in ("table_stride", "q_row_stride", "q_head_stride", "out_row_stride", "out_head_stride")] + [
         (n, C.c_int32) for n in ("q_type", "n_rows", "n_seqs", "max_blocks", "n_q_heads", "max_rows", "max_len")] + [
-        ("scale", C.c_float)]
+        ("scale", C.c_float), ("status", C.c_void_p), ("inject_short_copy", C.c_int32)]
 
 
 class SampleArgs(C.Structure):
@@ -326,15 +327,16 @@ def paged_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cach
 def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor, seq_len: torch.Tensor,
                     *, row_start: torch.Tensor | None = None, max_rows: int = 0, max_len: int = 0, scale: float = 0.0, k_scale=None,
                     v_scale=None, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
-                    scratch: torch.Tensor | None = None) -> torch.Tensor:
+                    scratch: torch.Tensor | None = None, status: torch.Tensor | None = None) -> torch.Tensor:
     """sparsk_paged_attention: rows q [n, n_q_heads, head_dim] (bf16 or fp16) of sequences whose seq_len (int32, new rows
     included) positions lie in the pages of block_table (int32 [sequences, blocks]).  Sequence i has rows row_start[i]
     to row_start[i + 1] - 1; without row_start every sequence has one.  max_rows and max_len, where known, size the launch.  `lse`
-    (float32 [n, n_q_heads]) receives the logarithms of the softmax sums."""
+    (float32 [n, n_q_heads]) receives the logarithms of the softmax sums.  Rows whose kernel had to give up waiting are NaN, and `status`
+    (int32 [1], never cleared here) then gets PAGED_TIMEOUT."""
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     (_paged or _native()).paged_attention(q, k_cache, v_cache, block_table, seq_len, row_start, max_rows, max_len, scale, k_scale,
-                                          v_scale, out, lse, scratch)
+                                          v_scale, out, lse, scratch, status)
     return out
 
 

@@ -63,7 +63,7 @@ bool paged_attn_ok(const sparsk_paged_attn_args *a)
     if (!a || !pool_ok(a->pool) || a->pool.page_size % 16) return false;
     if (a->q_type != SPARSK_BF16 && !(a->q_type == SPARSK_FP16 && a->pool.type != SPARSK_BF16)) return false;
     if (a->n_rows < 0 || a->n_seqs < 1 || a->max_blocks < 1 || a->n_q_heads < 1 || a->n_q_heads % a->pool.n_kv_heads) return false;
-    if (a->max_rows < 0 || a->max_len < 0 || (!a->row_start && a->n_rows != a->n_seqs)) return false;
+    if (a->max_rows < 0 || a->max_len < 0 || a->inject_short_copy < 0 || (!a->row_start && a->n_rows != a->n_seqs)) return false;
     if (!(a->scale >= 0.f) || !(a->scale < INFINITY)) return false;
     if (a->table_stride < a->max_blocks || a->table_stride > INT_MAX) return false;
     if ((int64_t)a->max_blocks * a->pool.page_size > INT_MAX - 64 || (int64_t)a->n_rows * a->n_q_heads > INT_MAX / 2) return false;
@@ -140,7 +140,7 @@ extern "C" int sparsk_paged_attention(const sparsk_paged_attn_args *a, void *scr
 {
     if (!paged_attn_ok(a) || !a->q || !a->out || !a->block_table || !a->seq_len || !scratch || !aligned(scratch, 256)) return SPARSK_EINVAL;
     if (!aligned(a->q, 2) || !aligned(a->out, 2) || !aligned(a->lse, 4) || !aligned(a->block_table, 4) || !aligned(a->seq_len, 4) ||
-        !aligned(a->row_start, 4))
+        !aligned(a->row_start, 4) || !aligned(a->status, 4))
         return SPARSK_EINVAL;
     const Scratch sc = scratch_of(a);
     if (scratch_bytes < sc.bytes) return SPARSK_EINVAL;
@@ -154,6 +154,7 @@ extern "C" int sparsk_paged_attention(const sparsk_paged_attn_args *a, void *scr
     p.block_table = a->block_table; p.seq_len = a->seq_len; p.row_start = a->row_start;
     p.k_scale = a->pool.k_scale; p.v_scale = a->pool.v_scale;
     p.records = (PtRecord *)scratch;
+    p.status = a->status; p.short_copy = a->inject_short_copy;
     p.part_ml = (float2 *)((char *)scratch + sc.ml);
     p.part_o = (float4 *)((char *)scratch + sc.o);
     p.table_stride = a->table_stride;

@@ -70,6 +70,7 @@ struct PtArgs {
     PtRecord *records;  // [shares]
     float4 *part_o;     // [shares][2][tiles][HD / 8][32 lanes]: accumulators as the lanes hold them
     float2 *part_ml;    // [shares][2][tiles][16]: maximum in powers of two, sum
+    int *status;        // or NULL
     long long table_stride, q_row_stride, q_head_stride, out_row_stride, out_head_stride;
     float scale_log2;
     float up;           // PtForm::UP
@@ -77,6 +78,7 @@ struct PtArgs {
     int tiles;          // of 16 query vectors, in a segment at most (1, 2 or 4)
     int page_shift;     // a page has 2^page_shift boxes, or -1
     int whole_boxes;    // segments of up to so many boxes are never cut
+    int short_copy;     // of which CTA (from 1) the stages wait for more bytes than come; 0: of none
     uint32_t g_inverse, g_limit;  // ceil(2^32 / G), and below which numbers it divides by G exactly
     int q_wide, out_words;      // queries may be read sixteen bytes at a time, outputs written two numbers at a time
 };
@@ -292,6 +294,8 @@ __device__ __forceinline__ long long pt_div(long long x, int y)
 {
     return (x >> 32) == 0 ? (long long)((unsigned)x / (unsigned)y) : pt_div_wide(x, y);
 }
+// a CTA's share of the sum of all costs
+__device__ __forceinline__ long long pt_share(long long total) { return max(pt_div(total + gridDim.x - 1, gridDim.x), (long long)PT_MIN_SHARE); }
 // v / G for a query vector's number
 __device__ __forceinline__ int pt_row_of(const PtArgs &a, int v)
 {
@@ -324,6 +328,9 @@ __device__ __forceinline__ bool pt_wait(uint64_t *bar, uint32_t parity, volatile
         }
     }
 }
+
+// A warp that is done (its copies have landed) and leaves; those that compute wait for all.
+__device__ __forceinline__ void pt_left() { asm volatile("barrier.arrive 1, %0;" ::"n"(PT_THREADS) : "memory"); }
 
 // The outputs of one vector from two neighbouring products: two and two numbers side by side, or, where the products took
 // even and odd dimensions (8-bit pages), four.
@@ -442,6 +449,7 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
                 else mbar_arrive(&q_full[slot]);
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
+            pt_left();
             return;
         }
         // ---------------------------------------------------------------- the warp that brings the boxes
@@ -452,7 +460,7 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
             if (lane >= o) upto += y;
         }
         const long long total = __shfl_sync(0xffffffffu, upto, PT_THREADS / 32 - 1);
-        const long long share = max(pt_div(total + gridDim.x - 1, gridDim.x), (long long)PT_MIN_SHARE);
+        const long long share = pt_share(total);
         const long long beg = share * blockIdx.x, end = min(beg + share, total);
         int seq = 0, base = 0, it = 0, issued = 0, flags = 0, segs = 0;
         long long at = 0, x = beg;
@@ -560,7 +568,7 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
                     d.len = now.len;
                     d.qblk = qblk;
                     d.head = head;
-                    mbar_expect_tx(&full[st], (uint32_t)__popc(have) * 2u * PT_BOX * RB);
+                    mbar_expect_tx(&full[st], (uint32_t)__popc(have) * 2u * PT_BOX * RB + (a.short_copy == (int)blockIdx.x + 1 ? 16u : 0u));
                 }
                 __syncwarp();
                 if (copy) {
@@ -590,6 +598,7 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
         // someone has given up: no copy may land in shared memory that is another CTA's by then
         if (!ok)
             for (int k = max(0, issued - NS); k < issued; k++) pt_wait(&full[k % NS], (k / NS) & 1, giving_up + 1);
+        pt_left();
         return;
     }
 
@@ -612,7 +621,7 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
     };
     for (int it = 0;; it++) {
         const int st = it % NS;
-        if (!pt_wait(&full[st], (it / NS) & 1, giving_up)) return;
+        if (!pt_wait(&full[st], (it / NS) & 1, giving_up)) break;
         const PtStage d = stages[st];
         if (d.flags & PT_STOP) break;
         const int n_vec = d.rows * a.G;  // of the sequence
@@ -641,7 +650,7 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
             }
             // (the rows of vectors that a tile does not have hold anything, and nobody reads what comes of them)
             const int slot = segs & (q_slots - 1);
-            if (!pt_wait(&q_full[slot], (segs >> q_shift) & 1, giving_up)) return;
+            if (!pt_wait(&q_full[slot], (segs >> q_shift) & 1, giving_up)) break;
             segs++;
             const unsigned char *Q = queries + (slot * a.tiles + mt) * F::QTILE;
 #pragma unroll
@@ -890,10 +899,46 @@ paged_attn_kernel(const PtArgs a, const __grid_constant__ CUtensorMap mk, const 
             return true;
         };
         if (PG == 4) {
-            if (!finish(std::integral_constant<int, 4>{})) return;
+            if (!finish(std::integral_constant<int, 4>{})) break;
         } else if (PG == 2) {
-            if (!finish(std::integral_constant<int, 2>{})) return;
+            if (!finish(std::integral_constant<int, 2>{})) break;
         } else finish(std::integral_constant<int, 1>{});
+    }
+    asm volatile("barrier.sync 1, %0;" ::"n"(PT_THREADS) : "memory");
+    if (giving_up[0] == 0) return;
+
+    // -------------------------------------------------------------------- given up
+    // Every segment that this share has a part of becomes NaN: here, and through NaN partials in what the join makes of it.  (The
+    // records may lack what the share had not come to, so that the join takes partials of other segments along, or is not called for
+    // a segment that begins here: either way it writes NaN or nothing.)
+    if (tid == 0 && a.status) atomicOr(a.status, SPARSK_PAGED_TIMEOUT);
+    if (tid < 2 * a.tiles * 16) a.part_ml[(size_t)blockIdx.x * 2 * a.tiles * 16 + tid] = make_float2(-INFINITY, __int_as_float(0x7fffffff));
+    long long total = 0, at = 0;
+#pragma unroll 1
+    for (int i = 0; i < a.n_seqs; i++) {
+        const PtSeq s = pt_seq(a, i);
+        total += (long long)pt_segments(a, s.rows) * cost_of(s);
+    }
+    const long long share = pt_share(total), beg = share * blockIdx.x, end = min(beg + share, total);
+#pragma unroll 1
+    for (int i = 0; i < a.n_seqs && at < end; i++) {
+        const PtSeq s = pt_seq(a, i);
+        const int cost = cost_of(s), boxes = boxes_of(s), each = box_cost(s), n_segs = pt_segments(a, s.rows);
+#pragma unroll 1
+        for (long long g = at < beg ? min(pt_div(beg - at, cost), (long long)n_segs) : 0; g < n_segs && at + g * cost < end; g++) {
+            const long long first = at + g * cost;
+            const int from = (int)max(beg - first, 0ll), to = (int)min(end - first, (long long)cost);
+            const int b0 = min((from + each - 1) / each, boxes), b1 = min((to + each - 1) / each, boxes);
+            if (boxes <= a.whole_boxes ? from > 0 : b0 >= b1 && !(boxes == 0 && from == 0)) continue;
+            const int qblk = (int)(g / a.Hk), head = (int)(g % a.Hk), v0 = qblk * a.tiles * 16, n = min(s.rows * a.G - v0, a.tiles * 16);
+#pragma unroll 1
+            for (int k = tid; k < n * HD; k += PT_WARPS * 32) {
+                const int v = v0 + k / HD, r = v / a.G, h = head * a.G + v % a.G;
+                reinterpret_cast<uint16_t *>(a.out)[(s.row0 + r) * a.out_row_stride + h * a.out_head_stride + k % HD] = 0x7fff;  // (bf16 and fp16)
+                if (a.lse && k % HD == 0) a.lse[(long long)(s.row0 + r) * a.Hk * a.G + h] = __int_as_float(0x7fffffff);
+            }
+        }
+        at += (long long)n_segs * cost;
     }
 }
 

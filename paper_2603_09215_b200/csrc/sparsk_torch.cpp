@@ -235,10 +235,10 @@ PyObject *paged_append(PyObject *, PyObject *const *x, Py_ssize_t n_args)
     });
 }
 
-// (q, k_cache, v_cache, block_table, seq_len, row_start, max_rows, max_len, scale, k_scale, v_scale, out, lse, scratch)
+// (q, k_cache, v_cache, block_table, seq_len, row_start, max_rows, max_len, scale, k_scale, v_scale, out, lse, scratch, status)
 PyObject *paged_attention(PyObject *, PyObject *const *x, Py_ssize_t n_args)
 {
-    return guarded(n_args, 14, [&] {
+    return guarded(n_args, 15, [&] {
         sparsk_paged_attn_args a{};
         const int dev = pool_of(x[1], x[2], x[9], x[10], a.pool);
         const at::Tensor &q = tensor(x[0], "q"), &out = tensor(x[11], "out"), &lens = tensor(x[4], "seq_len");
@@ -260,6 +260,7 @@ PyObject *paged_attention(PyObject *, PyObject *const *x, Py_ssize_t n_args)
             refuse("scale: a number is wanted");
         }
         a.scale = (float)scale;
+        a.status = array<int32_t>(x[14], at::kInt, 1, dev, "status", true);
         if (n == 0) return;
         at::Tensor own;  // (held until the launch; then the stream's order keeps it)
         void *scratch;

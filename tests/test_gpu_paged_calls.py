@@ -1,5 +1,7 @@
 """Calls of the paged operators that their documentation allows, or that have to be refused, and that can go wrong in ways of their
 own (references in 64 bits: tests/paged_util.py)."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -87,3 +89,52 @@ def test_light_positions_behind_a_sink(B, qt, cache, gap):
         vc[int(table[i, 0])], vc[int(table[i, 1])] = 0.0, 0.0
     base.check_attn(B, q, kc, vc, table, lens, start, [None, None], max_rows=2, max_len=3000)
     base.check_attn(B, q, kc, vc, table, lens, start, [None, None])
+
+
+@pytest.mark.parametrize("lens,rows,hq,hk,hd,qt,cache,nth,hint", [
+    ([20000], [1], 8, 2, 64, BF, FP, 40, 0),             # two segments cut into many shares: partials that are joined
+    ([100] * 300, [1] * 300, 8, 2, 128, FP, FP, 7, 100),   # short segments, several to a share, none cut
+    ([900, 4000, 33, 0, 2500] * 8, [4, 1, 3, 1, 2] * 8, 32, 2, 128, BF, E4, 100, 0),
+    ([5], [1], 4, 2, 64, BF, BF, 1, 5),
+])
+def test_a_wait_that_runs_out(B, lens, rows, hq, hk, hd, qt, cache, nth, hint):
+    """One CTA's stages wait for bytes that do not come (two seconds, and two more for the copies to have landed).  The call ends, its
+    status says so, and every row is either what it always is or NaN; the next call is as if nothing had been."""
+    q, kc, vc, table, start, _ = base.attn_case(lens, rows, hq, hk, hd, 16, qt, cache, "hnd", nth)
+    L, t, n, s = B.load(), ints(table), ints(lens), ints(start)
+    new = lambda: (torch.full(q.shape, 5.0, dtype=q.dtype, device="cuda"), torch.full(q.shape[:2], 5.0, device="cuda"))  # noqa: E731
+    status = ints([0])
+    a = B.PagedAttnArgs()
+    a.pool.k, a.pool.v = kc.data_ptr(), vc.data_ptr()
+    a.pool.page_stride, a.pool.head_stride, a.pool.pos_stride = kc.stride()[:3]
+    types = {BF: B.BF16, FP: B.FP16, E4: B.E4M3}
+    a.pool.type, a.q_type = types[cache], types[qt]
+    a.pool.n_pages, a.pool.n_kv_heads, a.pool.page_size, a.pool.head_dim = kc.shape
+    a.q, a.block_table, a.seq_len, a.row_start = q.data_ptr(), t.data_ptr(), n.data_ptr(), s.data_ptr()
+    a.table_stride, a.max_blocks = table.shape[1], table.shape[1]
+    a.q_row_stride = a.out_row_stride = hq * hd
+    a.q_head_stride = a.out_head_stride = hd
+    a.n_rows, a.n_seqs, a.n_q_heads, a.max_len = len(q), len(lens), hq, hint
+    nbytes = L.sparsk_paged_attention_scratch_bytes(ctypes.addressof(a))
+    scratch = torch.full((nbytes,), 0x55, dtype=torch.uint8, device="cuda")
+
+    def run(inject, with_status=True):
+        out, lse = new()
+        a.out, a.lse, a.status, a.inject_short_copy = out.data_ptr(), lse.data_ptr(), status.data_ptr() if with_status else None, inject
+        assert L.sparsk_paged_attention(ctypes.addressof(a), scratch.data_ptr(), nbytes, torch.cuda.current_stream().cuda_stream) == B.OK
+        torch.cuda.synchronize()
+        return out, lse
+
+    want, want_lse = run(0)
+    assert int(status) == 0 and not bool(want.isnan().any()) and not bool(want_lse.isnan().any())
+    assert torch.equal(B.paged_attention(q, kc, vc, t, n, row_start=s, max_len=hint, status=status), want) and int(status) == 0
+    got, got_lse = run(nth)
+    assert int(status) == B.PAGED_TIMEOUT
+    lost = got.isnan().all(-1)
+    assert bool(lost.any()) and torch.equal(lost, got.isnan().any(-1)) and torch.equal(lost, got_lse.isnan())
+    assert torch.equal(got[~lost], want[~lost]) and torch.equal(got_lse[~lost], want_lse[~lost])
+    got, got_lse = run(0)
+    assert torch.equal(got, want) and torch.equal(got_lse, want_lse) and int(status) == B.PAGED_TIMEOUT  # (the caller clears it)
+    if len(lens) == 1:
+        status.zero_()
+        assert bool(run(nth, with_status=False)[0].isnan().any()) and int(status) == 0
