@@ -1,6 +1,10 @@
-"""Compile the CUDA library (sm_100a) and the torch marshalling of its paged calls in-tree: ``python -m paper_2603_09215_b200.build``."""
+"""Compile the CUDA library (sm_100a) and the torch marshalling of its paged calls in-tree: ``python -m paper_2603_09215_b200.build``.
+
+The library needs nvcc alone, and is built whatever becomes of the marshalling: callers of the C ABI have no use for that.  Without torch it
+is left out; where torch is there and it does not compile, that is an error, raised when the library is in its place."""
 from __future__ import annotations
 
+import importlib.util
 import os
 import subprocess
 import sys
@@ -13,10 +17,15 @@ PAGED = os.path.join(HERE, "_paged.so")
 SOURCES = ["sparsk_api.cu", "sparsk_ops.cu", "sparsk_noalloc.cu", "sparsk_paged.cu", "sparsk_paged_attn.cu"]
 
 
+def _have_torch() -> bool:
+    return importlib.util.find_spec("torch") is not None
+
+
 def _stale() -> bool:
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)]
     deps.append(os.path.join(os.path.dirname(HERE), "include", "sparsk.h"))
-    return any(not os.path.exists(so) or os.path.getmtime(p) > os.path.getmtime(so) for so in (LIB, PAGED) for p in deps)
+    made = (LIB, PAGED) if _have_torch() else (LIB,)
+    return any(not os.path.exists(so) or os.path.getmtime(p) > os.path.getmtime(so) for so in made for p in deps)
 
 
 def _paged_command() -> list[str]:
@@ -40,12 +49,25 @@ def build(force: bool = False, verbose: bool = False) -> str:
         cmd += ["-Xptxas", "-v"]
     cmd += [os.path.join(CSRC, s) for s in SOURCES]
     cmd += ["-lcuda"]
-    side = _paged_command()
-    with subprocess.Popen(side) as p:  # beside the CUDA sources
-        subprocess.run(cmd, check=True)
-    if p.returncode:
-        raise subprocess.CalledProcessError(p.returncode, side)
+    with subprocess.Popen(cmd) as lib:
+        problem = _build_paged()  # beside the CUDA sources
+    if lib.returncode:
+        raise subprocess.CalledProcessError(lib.returncode, cmd)
+    if problem:
+        raise RuntimeError(f"{LIB} is built, but {PAGED}, which the Python binding's paged calls need, is not: {problem}")
     return LIB
+
+
+def _build_paged() -> str | None:
+    """What went wrong, if something did."""
+    if not _have_torch():
+        print(f"no torch here: {PAGED}, which only the Python binding needs, is left out", file=sys.stderr)
+        return None
+    try:
+        subprocess.run(_paged_command(), check=True)
+    except Exception as e:  # (an import of torch that fails can raise anything)
+        return str(e)
+    return None
 
 
 if __name__ == "__main__":
