@@ -260,6 +260,7 @@ PyObject *paged_attention(PyObject *, PyObject *const *x, Py_ssize_t n_args)
             refuse("scale: a number is wanted");
         }
         a.scale = (float)scale;
+        if (scale != 0 && a.scale == 0.f) refuse("scale: too small for fp32, where 0 stands for 1 / sqrt(head_dim)");
         a.status = array<int32_t>(x[14], at::kInt, 1, dev, "status", true);
         if (n == 0) return;
         at::Tensor own;  // (held until the launch; then the stream's order keeps it)

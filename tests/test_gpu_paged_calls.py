@@ -138,3 +138,13 @@ def test_a_wait_that_runs_out(B, lens, rows, hq, hk, hd, qt, cache, nth, hint):
     if len(lens) == 1:
         status.zero_()
         assert bool(run(nth, with_status=False)[0].isnan().any()) and int(status) == 0
+
+
+def test_a_scale_that_fp32_does_not_hold_is_refused(B):
+    """Rounded to zero it would mean the default; the smallest that fp32 holds makes all weights equal."""
+    q, kc, vc, table, start, _ = base.attn_case([20], [1], 4, 2, 64, 16, FP, FP, "hnd", 1)
+    for scale in (1e-46, 1e-300, -1e-46):
+        with pytest.raises(B.SparskError) as e:
+            B.paged_attention(q, kc, vc, ints(table), ints([20]), scale=scale)
+        assert e.value.code == B.EINVAL
+    base.check_attn(B, q, kc, vc, table, [20], start, [None, None], scale=2e-38)
