@@ -431,7 +431,7 @@ int sparsk_paged_attention(const sparsk_paged_attn_args *args /*host*/, void *sc
  * cut, all ids.  The masses are exact to about 2^-40 of the whole and do not depend on the order in which the GPU adds them: the same
  * call draws the same token.  Logits are only read; rows lie row_stride elements apart.  Enqueued on `cuda_stream`;
  * SPARSK_EINVAL for NULL or misaligned pointers, sizes below one or an unknown type, SPARSK_ECAPACITY for more ids
- * than SPARSK_MAX_SAMPLE_IDS. */
+ * than SPARSK_MAX_SAMPLE_IDS, or rows whose CTAs (up to eight a row) are more than 2^31 - 1. */
 #define SPARSK_MAX_SAMPLE_IDS 262144
 typedef struct {
     const void *logits;        /* [n_rows][n_ids] of type SPARSK_FP32, SPARSK_BF16 or SPARSK_FP16 */

@@ -2,6 +2,7 @@
 // They run exactly the kernels a decode step runs, on caller-described inputs, so that one
 // stage can be driven, checked and profiled on its own.
 #include <algorithm>
+#include <climits>
 #include <cstdint>
 
 #include "../../include/sparsk.h"
@@ -143,6 +144,6 @@ extern "C" int sparsk_sample(const sparsk_sample_args *a, void *cuda_stream)
     for (const void *p : {(const void *)a->uniforms, (const void *)a->temperature, (const void *)a->top_p, (const void *)a->min_p,
                           (const void *)a->top_k, (const void *)a->id_lo, (const void *)a->id_hi, (const void *)a->token, (const void *)a->logprob})
         if ((uintptr_t)p % 4) return SPARSK_EINVAL;
-    if (a->n_ids > SPARSK_MAX_SAMPLE_IDS) return SPARSK_ECAPACITY;
+    if (a->n_ids > SPARSK_MAX_SAMPLE_IDS || (int64_t)a->n_rows * settings_ctas(a->n_ids) > INT_MAX) return SPARSK_ECAPACITY;
     return launch_settings_sample(*a, (cudaStream_t)cuda_stream) == cudaSuccess ? SPARSK_OK : SPARSK_ECUDA;
 }

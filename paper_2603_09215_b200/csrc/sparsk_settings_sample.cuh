@@ -828,12 +828,14 @@ static cudaError_t launch_settings_form(const sparsk_sample_args &a, cudaStream_
     cfg.numAttrs = C > 1 ? 1 : 0;
     return cudaLaunchKernelEx(&cfg, settings_sample_kernel<TYPE, C, T>, a);
 }
+inline int settings_ctas(int n_ids) { return n_ids <= 8192 ? 1 : n_ids <= 32768 ? 4 : 8; }  // of a row
 template <int TYPE>
 static cudaError_t launch_settings_type(const sparsk_sample_args &a, cudaStream_t st)
 {
     static_assert(SPARSK_MAX_SAMPLE_IDS <= 8 * 32768, "a CTA counts up to 65,535 ids a bin and holds 32,768");
-    if (a.n_ids <= 8192) return launch_settings_form<TYPE, 1, 512>(a, st);
-    if (a.n_ids <= 32768) return launch_settings_form<TYPE, 4, 512>(a, st);
+    const int ctas = settings_ctas(a.n_ids);
+    if (ctas == 1) return launch_settings_form<TYPE, 1, 512>(a, st);
+    if (ctas == 4) return launch_settings_form<TYPE, 4, 512>(a, st);
     return launch_settings_form<TYPE, 8, 256>(a, st);
 }
 inline cudaError_t launch_settings_sample(const sparsk_sample_args &a, cudaStream_t st)
