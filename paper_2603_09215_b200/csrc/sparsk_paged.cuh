@@ -5,6 +5,7 @@
 
 #include "../../include/sparsk.h"
 #include "sparsk_common.cuh"
+#include "sparsk_warp.cuh"
 
 namespace sparsk {
 
@@ -185,12 +186,6 @@ static __global__ void __launch_bounds__(PM_THREADS) page_map_kernel(const PageM
 // 28 (read number by number 23 and 33).
 constexpr int PA_THREADS = 256;
 
-// A number beyond the type's largest is stored as that (an infinity in the cache would make every later score
-// of its head NaN), NaN stays NaN; the conversion to e4m3 does the same of itself.
-__device__ __forceinline__ float pa_clamp_fp16(float x)
-{
-    return x > 65504.f ? 65504.f : (x < -65504.f ? -65504.f : x);  // (a comparison with NaN is false)
-}
 template <int TYPE>
 __device__ __forceinline__ void pa_store8(void *p, const float (&v)[8], bool vec)
 {

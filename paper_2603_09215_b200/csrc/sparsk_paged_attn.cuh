@@ -26,10 +26,12 @@
 // out of line, one code for all tile counts.
 #pragma once
 
-#include <cuda_fp8.h>
+#include <cstdint>
+#include <type_traits>
 
-#include "sparsk_attn.cuh"
-#include "sparsk_paged.cuh"
+#include "../../include/sparsk.h"
+#include "sparsk_common.cuh"
+#include "sparsk_warp.cuh"
 
 namespace sparsk {
 
