@@ -6,6 +6,7 @@ import numpy as np
 import pytest
 import torch
 
+from tests import paged_util as pu
 from tests import test_gpu_paged as base
 
 pytestmark = pytest.mark.gpu
@@ -148,3 +149,33 @@ def test_a_scale_that_fp32_does_not_hold_is_refused(B):
             B.paged_attention(q, kc, vc, ints(table), ints([20]), scale=scale)
         assert e.value.code == B.EINVAL
     base.check_attn(B, q, kc, vc, table, [20], start, [None, None], scale=2e-38)
+
+
+def test_no_page_is_lost_or_handed_out_twice(B):
+    """Requests that come, grow and end for many steps, steps that are refused among them: after each, the pages of the live sequences
+    and those of the queue are all pages, once each."""
+    n, page, pages, blocks, most = 7, 4, 40, 12, 64
+    rng = np.random.default_rng(3)
+    table = torch.full((n, blocks), -1, dtype=torch.int32, device="cuda")
+    ring = ints(np.concatenate([rng.permutation(pages), np.full(5, -1)]))
+    size = len(ring)
+    lens, queue, refused = ints([0] * n), ints([0, pages]), 0
+    for step in range(120):
+        rows = rng.integers(0, 7, n) - (rng.random(n) < 0.1) * 100
+        rows = np.maximum(rows, -1)
+        host = lens.tolist(), queue.tolist(), table.cpu().numpy(), ring.cpu().numpy()
+        want = pu.page_map(host[0], rows, host[2], host[3], host[1], page, most)
+        m = B.page_map(lens, ints(rows), table, ring, queue, page, max_rows=most)
+        assert (int(m.status) == 0) == (want is not None)
+        if want is None:
+            refused += 1
+            rows = np.where(rng.random(n) < 0.5, -1, 0)  # (room again)
+            want = pu.page_map(host[0], rows, host[2], host[3], host[1], page, most)
+            m = B.page_map(lens, ints(rows), table, ring, queue, page, max_rows=most)
+            assert int(m.status) == 0
+        lens, queue = m.seq_len, m.queue
+        assert lens.tolist() == want[2].tolist() and queue.tolist() == want[3].tolist()
+        t, r, (head, count) = table.tolist(), ring.tolist(), queue.tolist()
+        held = [t[i][b] for i, length in enumerate(lens.tolist()) for b in range(-(-length // page))]
+        assert sorted(held + [r[(head + k) % size] for k in range(count)]) == list(range(pages)), step
+    assert refused > 5
