@@ -828,7 +828,12 @@ static cudaError_t launch_settings_form(const sparsk_sample_args &a, cudaStream_
     cfg.numAttrs = C > 1 ? 1 : 0;
     return cudaLaunchKernelEx(&cfg, settings_sample_kernel<TYPE, C, T>, a);
 }
-inline int settings_ctas(int n_ids) { return n_ids <= 8192 ? 1 : n_ids <= 32768 ? 4 : 8; }  // of a row
+// CTAs of a row, by its ids: what is fastest for few rows.  us with top-p in one / four / eight CTAs, fp32:
+//              8,192               12,288              32,768              65,536              131,072 ids
+//   1 row      14.9  16.2  16.1    17.3  16.8  16.8    25.4  18.4  18.0       -  22.7  21.1       -  29.1  25.9
+//   64 rows    15.4  32.6  37.8    17.6  33.4  38.5    26.2  37.7  42.8       -  45.4  50.2       -  60.2  65.4
+// (Many rows would take fewer CTAs each up to 32,768 ids; the choice does not look at the rows.)
+inline int settings_ctas(int n_ids) { return n_ids <= 8192 ? 1 : n_ids <= 32768 ? 4 : 8; }
 template <int TYPE>
 static cudaError_t launch_settings_type(const sparsk_sample_args &a, cudaStream_t st)
 {
