@@ -428,7 +428,7 @@ int sparsk_paged_attention(const sparsk_paged_attn_args *args /*host*/, void *sc
  * kept mass.  A temperature of 0 (below 2^-126, or NaN) takes the first id of the order.  logprob[r] (may be
  * NULL) is the logarithm of the token's softmax(z / temperature) over all of the row's ids (temperature 1 where the first id is taken).
  * A row without ids gets -1 and minus infinity.  Settings are DEVICE arrays [n_rows]; NULL stands for temperature 1, no
- * cut, all ids.  The masses are exact to about 2^-40 of the whole and do not depend on the order in which the GPU adds them: the same
+ * cut, all ids.  The masses are exact to about 2^-35 of the whole and do not depend on the order in which the GPU adds them: the same
  * call draws the same token.  Logits are only read; rows lie row_stride elements apart.  Enqueued on `cuda_stream`;
  * SPARSK_EINVAL for NULL or misaligned pointers, sizes below one or an unknown type, SPARSK_ECAPACITY for more ids
  * than SPARSK_MAX_SAMPLE_IDS, or rows whose CTAs (up to eight a row) are more than 2^31 - 1. */

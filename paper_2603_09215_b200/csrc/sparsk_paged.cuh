@@ -179,11 +179,11 @@ static __global__ void __launch_bounds__(PM_THREADS) page_map_kernel(const PageM
 
 // ------------------------------------------------------------------ rows into pages
 // A thread takes eight pairs (j, j + head_dim / 2) of one head of one row: two 16-byte reads and two writes of a
-// 16-bit type, and the pairs' cosines and sines once.  Bound by bytes where there are many rows (every number is
-// read and written once), by latency in a decode step.  4,001 rows of 36 heads of 128 (bf16, 32 of them queries, into e4m3 pages): 74 MB
-// in 20.9 us (torch's copy of as many bytes: 26).  Four heads a thread, turned by the same factors: 20.7, two: 21.9; numbers asked
-// for only when it was known where they go: 23.4.  Rows that do not start at 16 bytes, rising positions: 21 us for 17.7, fp32
-// 28 (read number by number 23 and 33).
+// 16-bit type, and the pairs' cosines and sines once.  Every number is read and written once; what bounds it is latency, in a decode step
+// one trip after another, with many rows six waves of blocks whose threads wait for a row, its slot and the table's entry in turn.
+// 4,001 rows of 36 heads of 128 (bf16, 32 of them queries, into e4m3 pages): 74 MB in 20.9 us (11.3 at the rate of a large copy; torch's
+// copy of as many bytes 26).  Four heads a thread, turned by the same factors: 20.7, two: 21.9; numbers asked for only when it was
+// known where they go: 23.4.  Rows that do not start at 16 bytes, rising positions: 21 us for 17.7, fp32 28 (read number by number 23 and 33).
 constexpr int PA_THREADS = 256;
 
 template <int TYPE>

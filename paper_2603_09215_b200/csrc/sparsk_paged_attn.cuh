@@ -6,7 +6,7 @@
 // m16n8k16 products (as in sparsk_attn.cuh), so that one read of the head's keys and values serves all of them.
 // All segments, laid end to end in boxes of 16 positions (plus a few boxes' worth for a segment's set-up and end), are cut into equal
 // shares, one for each CTA of a grid that is resident at once: nobody knows the lengths but the device, and
-// one warp of every CTA adds them up.  A share begins and ends anywhere; a segment that lies in one share is written
+// every CTA adds them up.  A share begins and ends anywhere; a segment that lies in one share is written
 // out at once, others leave a partial (sums and maxima) at either end of a share, which
 // a second kernel joins in order.
 //
@@ -19,9 +19,13 @@
 // Bound by HBM where a segment has one tile of query vectors: a position of a head of 128 fp16 numbers is 512 bytes, 23 of which
 // come per clock and SM, so 16 positions may take 350 clocks of an SM; eight computing warps need about 240.  64 sequences of
 // 8,192 positions (32 heads on 2, bf16): 537 MB in 92 us, 5.8 TB/s of 6.5 that a copy reaches; 64 of 256 to 2,048 (28 on 4, fp16): 152 MB
-// in 35.2 us, of which the first copies take 3, the segments' ends and the join 5.  With three or four tiles the warps' instructions
+// in 35.8 us, of which the first copies take 3, the segments' ends and the join 5.  With three or four tiles the warps' instructions
 // bound it (about 330 a box and tile, widening of 8-bit pages among them): 48 refresh blocks of up to four rows, 32 heads on 2:
-// 60 MB of e4m3 in 47 us, 120 MB of fp16 in 41.  Two boxes side by side in a warp gave those 45 and 42, and cost single rows 4 %.
+// 60 MB of e4m3 in 45 us, 120 MB of fp16 in 42.  Two boxes side by side in a warp were 4 % faster there over e4m3, and slower
+// elsewhere (single rows 4 %).  Single rows over 8-bit pages are bound by instructions as well: half the bytes leave 175 clocks for 16
+// positions, and their numbers are widened besides: 64 sequences of 8,192 (32 on 2) 74 us, 41 of them bytes; fp16 92 of 82.
+// A block of vectors is sent every box of its sequence, those behind its last row too, which are masked: a refresh block has one or two
+// of them, but of the rows of a prompt from nothing half the boxes are such (four of 1,000 rows, 28 on 4: 734 us, 39 TFLOP/s).
 // What a share waits for at its start is instructions that no warp of the SM has met yet, more than memory: divisions
 // out of line, one code for all tile counts.
 #pragma once
@@ -97,7 +101,7 @@ struct PtForm {
     static constexpr int SMEM = NS * STAGE + MEET + 4 * QTILE + NS * (16 + (int)sizeof(PtStage)) + 160 + PT_WARPS * 16 * 8 + 16;
     static_assert(PT_CTAS * (SMEM + 1024) <= 228 * 1024, "two CTAs share an SM");
     // What a box costs where the segment has one tile of vectors (the stage's boxes go to four warps), two (two by two) or more
-    // (every box to every warp).  48 refresh blocks over e4m3 / fp16 pages, us: 2, 3, 5 47.2 / 41.3; 2, 3, 6 50.1 / 43.5; 2, 3, 8 56.6 / 49.9; 2,
+    // (every box to every warp).  48 refresh blocks over e4m3 / fp16 pages, us: 2, 3, 5 47.2 / 41.3 (44.8 / 42.3 since); 2, 3, 6 50.1 / 43.5; 2, 3, 8 56.6 / 49.9; 2,
     // 2, 5 56.5 / 48.4; 2, 4, 6 48.9 / 43.7 (and 28 vectors in fp16 56.1 for 51.9).
     static constexpr int PT_C2 = 3, PT_C4 = 5;
     static constexpr float UP = CT == SPARSK_BF16 ? 0.f : PT_UP;  // (bf16 weights have the range of fp32)
