@@ -179,3 +179,32 @@ def test_no_page_is_lost_or_handed_out_twice(B):
         held = [t[i][b] for i, length in enumerate(lens.tolist()) for b in range(-(-length // page))]
         assert sorted(held + [r[(head + k) % size] for k in range(count)]) == list(range(pages)), step
     assert refused > 5
+
+
+@pytest.mark.parametrize("scale", [0.5, 4.0, 10.0])
+@pytest.mark.parametrize("qt,cache", [(BF, FP), (FP, FP), (BF, E4), (FP, E4)])
+def test_weights_are_right_to_what_is_promised(B, qt, cache, scale):
+    """Scores far apart, every third position (the heaviest often among them) of zero values.  A weight may be off by its rounding,
+    2^-11, and by 2^-20 of the largest of the same 16 positions; a score by the fp32 sums of its products; numbers below fp32's normal
+    range are zero (2^-120 is far above what they can add up to)."""
+    lens, rows, page, hd, hq, hk = [1500, 17, 100, 333], [1, 4, 9, 2], 32, 64, 8, 2
+    q, kc, vc, table, start, _ = base.attn_case(lens, rows, hq, hk, hd, page, qt, cache, "nhd", 31)
+    for i, length in enumerate(lens):
+        for p in range(0, length, 3):
+            vc[int(table[i, p // page]), :, p % page] = 0.0
+    out = B.paged_attention(q, kc, vc, ints(table), ints(lens), row_start=ints(start), scale=scale).double().cpu().numpy()
+    qd, kd, vd = (t.double().cpu().numpy() for t in (q, kc, vc))
+    for i, (length, R) in enumerate(zip(lens, rows)):
+        for j in range(R):
+            p = np.arange(length - R + 1 + j)
+            k, v = (x[table[i, p // page], :, p % page] for x in (kd, vd))  # [position, head, dim]
+            first = np.arange(0, len(p), 16)
+            for h in range(hq):
+                kh, vh, x = k[:, h * hk // hq], v[:, h * hk // hq], qd[start[i] + j, h]
+                s = scale * kh @ x
+                w = np.exp(s - s.max())
+                want = w @ vh / w.sum()
+                d = scale * (np.abs(kh) @ np.abs(x)).max() * (hd + 8) * 2.0 ** -24 + 2.0 ** -20
+                tol = (w @ np.abs(vh)) / w.sum() * (2.0 ** -11 + 2 * d + (len(p) + 64) * 2.0 ** -24)
+                tol += 2.0 ** -20 * np.maximum.reduceat(w, first) @ np.add.reduceat(np.abs(vh), first) / w.sum() + 2.0 ** -120
+                assert (np.abs(out[start[i] + j, h] - want) <= tol + pu.half_step(qt) * (np.abs(want) + tol) + pu.TINY[qt]).all(), (i, j, h)
